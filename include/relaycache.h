@@ -421,6 +421,122 @@ RC_API rc_status rc_rope_scatter(const float* qkv, const int32_t* pos, int32_t n
 RC_API rc_status rc_scatter_paged(const void* k_rows, const void* v_rows, const int32_t* pos, int32_t n,
                            const rc_kv_layer* dst, int32_t seq, void* stream);
 
+/* --------------------------------------------------- ragged batches over a paged cache
+ * What a program needs that runs decoder layers of its own over these caches, several requests of any lengths in one call:
+ * rc_batch_map (once a step) turns the requests' lengths into block tables, slots and key ranges, rc_norm_rotary_rows
+ * (every layer) brings the projections into queries and cache rows, rc_masked_attention attends, and rc_rotary_move takes
+ * another agent's rows over.  The rows of a batch lie one behind the other, sequence by sequence; row_start [n_seq + 1] says where
+ * (row_start[s] .. row_start[s + 1] - 1 are those of sequence s).  All counts and indices are read from device memory, the host gives
+ * bounds for them: nothing is copied back, every call can be captured in a graph and replayed with other lengths inside
+ * the bounds.  Rows behind the last sequence's are left as they were.
+ * A slot names a row of a pool: block * block_size + (position % block_size).  A row with a slot outside the pool (-1) leaves the cache
+ * alone.  Two rows of one call with the same slot: which of them stays there is not defined. */
+
+/* Rotary positions of more kinds than a model's rope_base: pairs (i, i + rotary_dim/2) or (2i, 2i + 1) of the first rotary_dim elements of a head,
+ * the rest passes through; pair i turns by pos * freq[i], and both of its elements are multiplied by `amplitude`. */
+#define RC_ROTARY_MAX_PAIRS 64
+typedef enum { RC_ROTARY_HALF = 0, RC_ROTARY_INTERLEAVED = 1 } rc_rotary_layout;
+/* freq[i] = f = base^(-2i/rotary_dim), for contexts longer than the trained length:
+ *   LINEAR    f / factor
+ *   BY_TURNS  t = trained_len f / 2 pi, w = clamp((t - slow_turns) / (fast_turns - slow_turns), 0, 1):  w f + (1 - w) f / factor
+ *   BY_PAIR   w falls linearly with i, from 1 at the pair that turns fast_turns times over trained_len (rounded down) to 0 at the one
+ *             that turns slow_turns times (rounded up): the same mixture (the rule of arXiv 2309.00071, whose amplitude is
+ *             0.1 ln(factor) + 1) */
+typedef enum { RC_ROTARY_PLAIN = 0, RC_ROTARY_LINEAR = 1, RC_ROTARY_BY_TURNS = 2, RC_ROTARY_BY_PAIR = 3 } rc_rotary_scaling;
+typedef struct {
+  int32_t layout;      /* rc_rotary_layout */
+  int32_t rotary_dim;  /* a multiple of 8, at most 128 (and, where it is used, at most head_dim) */
+  int32_t scaling;     /* rc_rotary_scaling */
+  int32_t trained_len; /* BY_TURNS, BY_PAIR: >= 1 */
+  double base;         /* > 0; BY_PAIR: > 1 */
+  double factor;       /* LINEAR, BY_TURNS, BY_PAIR: > 0 */
+  double slow_turns, fast_turns; /* BY_TURNS, BY_PAIR: 0 < slow_turns < fast_turns */
+  double amplitude;    /* > 0 */
+} rc_rotary_desc;
+typedef struct {
+  int32_t layout, rotary_dim;
+  double amplitude;
+  double freq[RC_ROTARY_MAX_PAIRS];   /* a program may also fill these in itself */
+} rc_rotary;
+/* Host function: fills *out, a plain host struct that the calls below read during the call only. */
+RC_API rc_status rc_rotary_init(const rc_rotary_desc* desc, rc_rotary* out);
+
+/* Block tables, slots and key ranges of a step.  Sequence s holds n_cached[s] rows and gets n_new[s] more (0 is fine, a
+ * negative count is one).  Blocks that the new rows need are taken from free_blocks in the order of the sequences, starting at entry *free_first,
+ * and entered in the block table; the entries of blocks that a sequence has already stay as they are.
+ * A sequence is refused as a whole where its rows would not fit its block table, the free list or max_rows: it takes no block,
+ * its rows get slot -1 and see no key (lo 0, hi -1), the other sequences are served.  (Behind the one that the free list is too short for,
+ * only sequences that need no block are.)
+ * Keys that a row may see, both ends included: row_lo = first position of its document, row_hi = min(max(position,
+ * prefix_len - 1), last position of its document).
+ * Outputs may not be inputs' memory (kv_len is not n_cached, counts does not hold free_first), but for block_table. */
+typedef struct {
+  int32_t n_seq;               /* 1 .. 65536 */
+  int32_t max_rows;            /* rows that the row arrays have room for, >= 0 */
+  const int32_t* n_cached;     /* device [n_seq] */
+  const int32_t* n_new;        /* device [n_seq] */
+  int32_t* block_table;        /* device [n_seq][max_blocks_per_seq], in/out */
+  int32_t max_blocks_per_seq, block_size, n_blocks;   /* n_blocks * block_size < 2^31 */
+  int32_t n_free;
+  const int32_t* free_blocks;  /* device [n_free] (NULL with n_free 0) */
+  const int32_t* free_first;   /* device, optional: the first free entry; NULL: 0 */
+  const int32_t* prefix_len;   /* device [n_seq], optional: keys before it are seen by every row of the sequence */
+  const int32_t* doc_start;    /* device [n_seq + 1], optional: the documents of sequence s are doc_first[doc_start[s] .. doc_start[s + 1] - 1], */
+  const int32_t* doc_first;    /*   ascending positions at which a document begins (one begins at 0 in any case); device [n_docs], NULL with n_docs 0 */
+  int32_t n_docs;
+  int32_t* row_start;          /* out: device [n_seq + 1], at most max_rows each */
+  int32_t *row_seq, *row_pos, *row_slot, *row_lo, *row_hi;   /* out: device [max_rows]; each may be NULL */
+  int32_t* kv_len;             /* out: device [n_seq], rows that the sequence then holds; may be NULL */
+  int32_t* counts;             /* out: device [3]: rows of the batch, the next free entry, refused sequences; may be NULL */
+} rc_batch_map_args;
+RC_API rc_status rc_batch_map(const rc_batch_map_args* args, void* stream);
+
+/* What lies between a layer's q|k|v product and its attention, for rows of any sequences: row i of qkv [n][Hq*dh | Hkv*dh | Hkv*dh] (float, or bf16
+ * where qkv_dtype says so; rows qkv_stride elements apart, a multiple of 4) belongs to position pos[i] and slot[i].  Queries and keys
+ * are RMS-normalised head by head with the gains g_q, g_k [dh] of T (NULL: left as they are), x / sqrt(mean(x^2) + eps) * g,
+ * then rotated; queries go to q_out [n][Hq][dh] of T, keys and values into slot[i] of dst, keys before the rotation into slot[i] of the
+ * pool k_pre (optional, dst's geometry).  Sums and rotations are of 32 bits (angles of 64), and a result is rounded once.
+ * n_live (optional, device): rows that there are, where n is only a bound (rc_batch_map: row_start + n_seq).
+ * All arrays 16-byte aligned.  Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (stride, alignment, head_dim), RC_E_CAPACITY (pool of 2^31 rows). */
+RC_API rc_status rc_norm_rotary_rows(const void* qkv, int32_t qkv_dtype, int64_t qkv_stride, int32_t n, const int32_t* n_live,
+                                     int32_t n_q_heads, const void* g_q, const void* g_k, float eps, const rc_rotary* rotary,
+                                     const int32_t* pos, const int32_t* slot, const rc_kv_layer* dst, void* k_pre, void* q_out,
+                                     void* stream);
+
+/* Rows of one layer's cache moved to other slots and positions, of any sequences at once: row i goes from src_slot[i] of src to
+ * dst_slot[i] of dst, its key rotated from old_pos[i] to new_pos[i] (old_pos NULL: keys stored before rotation, rotated to new_pos[i] and
+ * multiplied by the amplitude, which rotated keys have already), its value copied.  src and dst have equal n_kv_heads, head_dim, dtype and may be one cache if
+ * every row of the call stays in its slot or no row's destination is another's source.  n_live as above. */
+RC_API rc_status rc_rotary_move(const rc_kv_layer* src, const int32_t* src_slot, const rc_kv_layer* dst, const int32_t* dst_slot,
+                                int32_t n, const int32_t* n_live, const rc_rotary* rotary, const int32_t* new_pos,
+                                const int32_t* old_pos, void* stream);
+
+/* Grouped-query attention of a ragged batch over one layer of a cache.  Query row i (already rotated) of sequence s sees the keys row_lo[i] ..
+ * row_hi[i] of block-table row seq[s], and no others (one that sees none gets zeros):
+ *   score = scale q.k, or cap tanh(scale q.k / cap);  score -= slopes[head] |row_pos[i] - key|;  out = softmax(score) V
+ * Key ranges are cut to [0, max_len).  Causal attention is row_lo NULL (0) and row_hi NULL (row_pos); sliding windows, documents and prefixes are ranges
+ * (rc_batch_map).  Keys and values outside a row's range do not touch it, whatever they hold.  q, out: [n_rows][Hq][dh] of T.
+ * workspace (optional, device, 256-byte aligned, rc_masked_attention_workspace_bytes): lets long key ranges be cut where the batch has few rows; NULL: not cut.
+ * Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (more than 128 query heads on a key head, alignment), RC_E_CAPACITY (max_len beyond the block table, n_seq),
+ * RC_E_WORKSPACE. */
+typedef struct {
+  int32_t n_seq;               /* 1 .. 65536 */
+  int32_t n_rows;              /* rows of q and out; row_start[n_seq] is at most that */
+  int32_t max_rows_per_seq;    /* no sequence has more rows (rows beyond are left as they were) */
+  int32_t max_len;             /* no sequence is looked at beyond, >= 1 */
+  const int32_t* row_start;    /* device [n_seq + 1] */
+  const int32_t* row_pos;      /* device [n_rows] */
+  const int32_t* row_lo;       /* device [n_rows], optional */
+  const int32_t* row_hi;       /* device [n_rows], optional */
+  const int32_t* seq;          /* device [n_seq], optional: row of the block table; NULL: s */
+  const float* slopes;         /* device [n_q_heads], optional */
+  float scale;                 /* 0: 1 / sqrt(head_dim) */
+  float cap;                   /* 0: none */
+} rc_masked_attention_args;
+RC_API size_t rc_masked_attention_workspace_bytes(const rc_masked_attention_args* args, int32_t n_q_heads, const rc_kv_layer* cache);
+RC_API rc_status rc_masked_attention(const void* q, const rc_masked_attention_args* args, int32_t n_q_heads, const rc_kv_layer* cache,
+                                     void* out, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

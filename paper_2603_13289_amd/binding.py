@@ -21,6 +21,9 @@ RC_OK, RC_E_INVALID_ARG, RC_E_UNSUPPORTED, RC_E_WORKSPACE, RC_E_HIP, RC_E_CAPACI
 RC_F32, RC_BF16 = 0, 1
 RC_MAX_REQ = 32
 RC_SELECT_BUDGET, RC_SELECT_THRESHOLD = 0, 1
+RC_ROTARY_HALF, RC_ROTARY_INTERLEAVED = 0, 1
+RC_ROTARY_PLAIN, RC_ROTARY_LINEAR, RC_ROTARY_BY_TURNS, RC_ROTARY_BY_PAIR = 0, 1, 2, 3
+RC_ROTARY_MAX_PAIRS = 64
 
 EXPORTS = [
     "rc_status_str", "rc_build_info", "rc_model_create", "rc_model_destroy", "rc_reuse_workspace_bytes",
@@ -31,6 +34,8 @@ EXPORTS = [
     "rc_tune_set", "rc_sparse_attention_workspace_bytes",
     "rc_gemm_workspace_bytes", "rc_rope_rerotate_static", "rc_rope_rerotate_static_scratch_bytes",
     "rc_rope_scatter", "rc_rope_scatter_workspace_bytes",
+    "rc_rotary_init", "rc_batch_map", "rc_norm_rotary_rows", "rc_rotary_move", "rc_masked_attention",
+    "rc_masked_attention_workspace_bytes",
 ]
 
 
@@ -86,6 +91,30 @@ class rc_plan(C.Structure):
     _fields_ = [("l_start", C.c_int32), ("l_det", C.c_int32), ("l_end", C.c_int32),
                 ("k_per_req", C.POINTER(C.c_int32)), ("forced_idx", C.c_void_p),
                 ("selector", C.c_int32), ("tau_dev", C.c_float), ("tau_inf", C.c_float), ("k_suf", C.c_int32)]
+
+
+class rc_rotary_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("layout", "rotary_dim", "scaling", "trained_len")] + \
+               [(n, C.c_double) for n in ("base", "factor", "slow_turns", "fast_turns", "amplitude")]
+
+
+class rc_rotary(C.Structure):
+    _fields_ = [("layout", C.c_int32), ("rotary_dim", C.c_int32), ("amplitude", C.c_double),
+                ("freq", C.c_double * RC_ROTARY_MAX_PAIRS)]
+
+
+class rc_batch_map_args(C.Structure):
+    _fields_ = [("n_seq", C.c_int32), ("max_rows", C.c_int32), ("n_cached", C.c_void_p), ("n_new", C.c_void_p),
+                ("block_table", C.c_void_p), ("max_blocks_per_seq", C.c_int32), ("block_size", C.c_int32),
+                ("n_blocks", C.c_int32), ("n_free", C.c_int32), ("free_blocks", C.c_void_p), ("free_first", C.c_void_p),
+                ("prefix_len", C.c_void_p), ("doc_start", C.c_void_p), ("doc_first", C.c_void_p), ("n_docs", C.c_int32)] + \
+               [(n, C.c_void_p) for n in ("row_start", "row_seq", "row_pos", "row_slot", "row_lo", "row_hi", "kv_len", "counts")]
+
+
+class rc_masked_attention_args(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_seq", "n_rows", "max_rows_per_seq", "max_len")] + \
+               [(n, C.c_void_p) for n in ("row_start", "row_pos", "row_lo", "row_hi", "seq", "slopes")] + \
+               [("scale", C.c_float), ("cap", C.c_float)]
 
 
 def _load() -> C.CDLL:
@@ -161,6 +190,20 @@ def _load() -> C.CDLL:
     lib.rc_gemm_workspace_bytes.argtypes = []
     lib.rc_scatter_paged.restype = C.c_int
     lib.rc_scatter_paged.argtypes = [vp, vp, vp, i32, C.POINTER(rc_kv_layer), i32, vp]
+    lib.rc_rotary_init.restype = C.c_int
+    lib.rc_rotary_init.argtypes = [C.POINTER(rc_rotary_desc), C.POINTER(rc_rotary)]
+    lib.rc_batch_map.restype = C.c_int
+    lib.rc_batch_map.argtypes = [C.POINTER(rc_batch_map_args), vp]
+    lib.rc_norm_rotary_rows.restype = C.c_int
+    lib.rc_norm_rotary_rows.argtypes = [vp, i32, C.c_int64, i32, vp, i32, vp, vp, C.c_float, C.POINTER(rc_rotary), vp, vp,
+                                        C.POINTER(rc_kv_layer), vp, vp, vp]
+    lib.rc_rotary_move.restype = C.c_int
+    lib.rc_rotary_move.argtypes = [C.POINTER(rc_kv_layer), vp, C.POINTER(rc_kv_layer), vp, i32, vp, C.POINTER(rc_rotary),
+                                   vp, vp, vp]
+    lib.rc_masked_attention_workspace_bytes.restype = sz
+    lib.rc_masked_attention_workspace_bytes.argtypes = [C.POINTER(rc_masked_attention_args), i32, C.POINTER(rc_kv_layer)]
+    lib.rc_masked_attention.restype = C.c_int
+    lib.rc_masked_attention.argtypes = [vp, C.POINTER(rc_masked_attention_args), i32, C.POINTER(rc_kv_layer), vp, vp, sz, vp]
     lib.rc_tune_set.restype = C.c_int
     lib.rc_tune_set.argtypes = [i32, i32]
     lib.rc_profile_enable.restype = C.c_int
@@ -575,6 +618,115 @@ def rc_scatter_paged(k_rows: torch.Tensor, v_rows: torch.Tensor, pos: torch.Tens
                      seq: int, stream=None) -> None:
     _check(lib.rc_scatter_paged(_ptr(k_rows), _ptr(v_rows), _ptr(pos), n, C.byref(dst), seq, _stream(stream)),
            "rc_scatter_paged")
+
+
+# ------------------------------------------------------------------ ragged batches over a paged cache
+def rc_rotary_init(layout: int, rotary_dim: int, base: float, scaling: int = RC_ROTARY_PLAIN, factor: float = 1.0,
+                   trained_len: int = 0, slow_turns: float = 1.0, fast_turns: float = 32.0,
+                   amplitude: float = 1.0) -> rc_rotary:
+    """Host function: the rotation's frequencies, a plain struct for rc_norm_rotary_rows and rc_rotary_move."""
+    desc = rc_rotary_desc(layout, rotary_dim, scaling, trained_len, base, factor, slow_turns, fast_turns, amplitude)
+    out = rc_rotary()
+    _check(lib.rc_rotary_init(C.byref(desc), C.byref(out)), "rc_rotary_init")
+    return out
+
+
+def _i32(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
+    if t is not None and (t.dtype != torch.int32 or t.numel() < n):
+        raise ValueError(f"{what}: {n} int32 values expected, got {t.numel()} of {t.dtype}")
+    return _ptr(t)
+
+
+@dataclass
+class BatchRows:
+    """What rc_batch_map writes: int32 device tensors, of one element per row (but row_start, kv_len, counts)."""
+    row_start: torch.Tensor                    # [n_seq + 1]
+    row_seq: Optional[torch.Tensor]
+    row_pos: Optional[torch.Tensor]
+    row_slot: Optional[torch.Tensor]
+    row_lo: Optional[torch.Tensor]
+    row_hi: Optional[torch.Tensor]
+    kv_len: Optional[torch.Tensor]             # [n_seq]
+    counts: Optional[torch.Tensor]             # [3]: rows, next free entry, refused sequences
+
+    @staticmethod
+    def alloc(n_seq: int, max_rows: int, device="cuda") -> "BatchRows":
+        z = lambda n: torch.zeros(n, dtype=torch.int32, device=device)
+        return BatchRows(z(n_seq + 1), *[z(max_rows) for _ in range(5)], z(n_seq), z(3))
+
+
+def rc_batch_map(n_cached: torch.Tensor, n_new: torch.Tensor, block_table: torch.Tensor, block_size: int, n_blocks: int,
+                 free_blocks: torch.Tensor, rows: BatchRows, free_first: Optional[torch.Tensor] = None,
+                 prefix_len: Optional[torch.Tensor] = None, doc_start: Optional[torch.Tensor] = None,
+                 doc_first: Optional[torch.Tensor] = None, stream=None) -> None:
+    n_seq = int(n_new.numel())
+    per_row = [t for t in (rows.row_seq, rows.row_pos, rows.row_slot, rows.row_lo, rows.row_hi) if t is not None]
+    max_rows = min((int(t.numel()) for t in per_row), default=2 ** 31 - 1)
+    if block_table.dim() != 2 or block_table.shape[0] < n_seq or block_table.dtype != torch.int32:
+        raise ValueError(f"block_table: int32 [{n_seq}][blocks] expected")
+    a = rc_batch_map_args(n_seq, max_rows, _i32(n_cached, n_seq, "n_cached"), _ptr(n_new), _ptr(block_table), block_table.shape[1],
+                          block_size, n_blocks, free_blocks.numel(), _i32(free_blocks, 0, "free_blocks") or None,
+                          _i32(free_first, 1, "free_first"), _i32(prefix_len, n_seq, "prefix_len"),
+                          _i32(doc_start, n_seq + 1, "doc_start"), _i32(doc_first, 0, "doc_first"),
+                          0 if doc_first is None else doc_first.numel(), _i32(rows.row_start, n_seq + 1, "row_start"),
+                          _i32(rows.row_seq, 0, "row_seq"), _i32(rows.row_pos, 0, "row_pos"), _i32(rows.row_slot, 0, "row_slot"),
+                          _i32(rows.row_lo, 0, "row_lo"), _i32(rows.row_hi, 0, "row_hi"), _i32(rows.kv_len, n_seq, "kv_len"),
+                          _i32(rows.counts, 3, "counts"))
+    _check(lib.rc_batch_map(C.byref(a), _stream(stream)), "rc_batch_map")
+
+
+def rc_norm_rotary_rows(qkv: torch.Tensor, n: int, n_q_heads: int, rotary: rc_rotary, pos: torch.Tensor, slot: torch.Tensor,
+                        dst: rc_kv_layer, q_out: torch.Tensor, g_q: Optional[torch.Tensor] = None,
+                        g_k: Optional[torch.Tensor] = None, eps: float = 1e-5, k_pre: Optional[torch.Tensor] = None,
+                        n_live: Optional[torch.Tensor] = None, stream=None) -> None:
+    """qkv: [rows][width], float32 or bf16, rows any multiple of 4 elements apart."""
+    assert qkv.dim() == 2 and qkv.stride(1) == 1 and qkv.dtype in (torch.float32, torch.bfloat16)
+    dtype = RC_BF16 if qkv.dtype == torch.bfloat16 else RC_F32
+    _check(lib.rc_norm_rotary_rows(qkv.data_ptr(), dtype, qkv.stride(0), n, _i32(n_live, 1, "n_live"), n_q_heads, _ptr(g_q),
+                                   _ptr(g_k), eps, C.byref(rotary), _i32(pos, n, "pos"), _i32(slot, n, "slot"), C.byref(dst),
+                                   _ptr(k_pre), _ptr(q_out), _stream(stream)), "rc_norm_rotary_rows")
+
+
+def rc_rotary_move(src: rc_kv_layer, src_slot: torch.Tensor, dst: rc_kv_layer, dst_slot: torch.Tensor, n: int,
+                   rotary: rc_rotary, new_pos: torch.Tensor, old_pos: Optional[torch.Tensor] = None,
+                   n_live: Optional[torch.Tensor] = None, stream=None) -> None:
+    _check(lib.rc_rotary_move(C.byref(src), _i32(src_slot, n, "src_slot"), C.byref(dst), _i32(dst_slot, n, "dst_slot"), n,
+                              _i32(n_live, 1, "n_live"), C.byref(rotary), _i32(new_pos, n, "new_pos"),
+                              _i32(old_pos, n, "old_pos"), _stream(stream)), "rc_rotary_move")
+
+
+@dataclass
+class MaskedAttention:
+    """The rows of a ragged batch as rc_masked_attention takes them (int32 device tensors, slopes float32)."""
+    row_start: torch.Tensor                    # [n_seq + 1]
+    row_pos: torch.Tensor                      # [n_rows]
+    n_rows: int
+    max_rows_per_seq: int
+    max_len: int
+    row_lo: Optional[torch.Tensor] = None      # [n_rows]; None: 0
+    row_hi: Optional[torch.Tensor] = None      # [n_rows]; None: row_pos
+    seq: Optional[torch.Tensor] = None         # [n_seq] rows of the block table; None: 0, 1, ...
+    slopes: Optional[torch.Tensor] = None      # [n_q_heads]
+    scale: float = 0.0                         # 0: 1 / sqrt(head_dim)
+    cap: float = 0.0                           # 0: none
+
+    def c(self) -> rc_masked_attention_args:
+        n_seq = int(self.row_start.numel()) - 1
+        return rc_masked_attention_args(n_seq, self.n_rows, self.max_rows_per_seq, self.max_len, _i32(self.row_start, 1, "row_start"),
+                                        _i32(self.row_pos, self.n_rows, "row_pos"), _i32(self.row_lo, self.n_rows, "row_lo"),
+                                        _i32(self.row_hi, self.n_rows, "row_hi"), _i32(self.seq, n_seq, "seq"), _ptr(self.slopes),
+                                        self.scale, self.cap)
+
+
+def rc_masked_attention_workspace_bytes(rows: MaskedAttention, n_q_heads: int, cache: rc_kv_layer) -> int:
+    return int(lib.rc_masked_attention_workspace_bytes(C.byref(rows.c()), n_q_heads, C.byref(cache)))
+
+
+def rc_masked_attention(q: torch.Tensor, rows: MaskedAttention, n_q_heads: int, cache: rc_kv_layer, out: torch.Tensor,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.rc_masked_attention(_ptr(q), C.byref(rows.c()), n_q_heads, C.byref(cache), _ptr(out), _ptr(workspace), nbytes,
+                                   _stream(stream)), "rc_masked_attention")
 
 
 # ------------------------------------------------------------------ per-stage timing

@@ -3,6 +3,8 @@
 // decides which rows are active in which layer and enqueues launches.
 #include <algorithm>
 #include <climits>
+#include <cmath>
+#include <initializer_list>
 #include <new>
 #include <type_traits>
 #include <vector>
@@ -1347,6 +1349,168 @@ rc_status rc_scatter_paged(const void* k_rows, const void* v_rows, const int32_t
   else
     RC_HIP(launch_scatter_rows<float>((const float*)k_rows, (const float*)v_rows, pos, n, (float*)dst->k,
                                       (float*)dst->v, geom_of(*dst), seq, st));
+  return RC_OK;
+}
+
+// ------------------------------------------------------------------ ragged batches
+rc_status rc_rotary_init(const rc_rotary_desc* d, rc_rotary* out) {
+  if (!d || !out) return RC_E_INVALID_ARG;
+  const bool scaled = d->scaling != RC_ROTARY_PLAIN, by_len = d->scaling == RC_ROTARY_BY_TURNS || d->scaling == RC_ROTARY_BY_PAIR;
+  if (d->layout != RC_ROTARY_HALF && d->layout != RC_ROTARY_INTERLEAVED) return RC_E_INVALID_ARG;
+  if (d->scaling < RC_ROTARY_PLAIN || d->scaling > RC_ROTARY_BY_PAIR) return RC_E_INVALID_ARG;
+  if (d->rotary_dim < 1 || !(d->base > 0.0) || !std::isfinite(d->base) || !(d->amplitude > 0.0) || !std::isfinite(d->amplitude)) return RC_E_INVALID_ARG;
+  if (d->rotary_dim % 8 || d->rotary_dim > 2 * RC_ROTARY_MAX_PAIRS) return RC_E_UNSUPPORTED;
+  if (scaled && (!(d->factor > 0.0) || !std::isfinite(d->factor))) return RC_E_INVALID_ARG;
+  if (by_len && (d->trained_len < 1 || !(d->slow_turns > 0.0) || !(d->fast_turns > d->slow_turns) || !std::isfinite(d->fast_turns)))
+    return RC_E_INVALID_ARG;
+  if (d->scaling == RC_ROTARY_BY_PAIR && !(d->base > 1.0)) return RC_E_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925;
+  const int half = d->rotary_dim / 2;
+  // the pair that turns `turns` times over the trained length
+  auto pair_at = [&](double turns) { return d->rotary_dim * std::log(d->trained_len / (turns * two_pi)) / (2.0 * std::log(d->base)); };
+  double first = 0.0, width = 1.0;
+  if (d->scaling == RC_ROTARY_BY_PAIR) {
+    first = std::max(std::floor(pair_at(d->fast_turns)), 0.0);
+    width = std::max(std::min(std::ceil(pair_at(d->slow_turns)), half - 1.0) - first, 0.001);
+  }
+  *out = rc_rotary();
+  out->layout = d->layout;
+  out->rotary_dim = d->rotary_dim;
+  out->amplitude = d->amplitude;
+  for (int i = 0; i < half; ++i) {
+    const double f = std::pow(d->base, -2.0 * i / d->rotary_dim);
+    double keep = 1.0;   // how much of the frequency stays as it is
+    if (d->scaling == RC_ROTARY_LINEAR) keep = 0.0;
+    else if (d->scaling == RC_ROTARY_BY_TURNS) keep = (d->trained_len * f / two_pi - d->slow_turns) / (d->fast_turns - d->slow_turns);
+    else if (d->scaling == RC_ROTARY_BY_PAIR) keep = 1.0 - (i - first) / width;
+    keep = std::min(std::max(keep, 0.0), 1.0);
+    out->freq[i] = scaled ? keep * f + (1.0 - keep) * (f / d->factor) : f;
+  }
+  return RC_OK;
+}
+
+static rc_status rotary_arg(const rc_rotary* r, int head_dim, RotaryArg* out) {
+  if (!r || (r->layout != RC_ROTARY_HALF && r->layout != RC_ROTARY_INTERLEAVED) || r->rotary_dim < 1) return RC_E_INVALID_ARG;
+  if (r->rotary_dim % 8 || r->rotary_dim > head_dim) return RC_E_UNSUPPORTED;
+  out->layout = r->layout;
+  out->rotary_dim = r->rotary_dim;
+  out->amplitude = (float)r->amplitude;
+  for (int i = 0; i < RC_ROTARY_MAX_PAIRS; ++i) out->turns[i] = i < r->rotary_dim / 2 ? r->freq[i] / 6.283185307179586476925 : 0.0;
+  return RC_OK;
+}
+
+static bool aligned16(std::initializer_list<const void*> ps) {
+  uintptr_t all = 0;
+  for (const void* p : ps) all |= reinterpret_cast<uintptr_t>(p);
+  return (all & 15u) == 0;
+}
+
+static rc_status slot_geom_of(const rc_kv_layer& kv, SlotGeom* g) {
+  if ((long)kv.n_blocks * kv.block_size > INT_MAX) return RC_E_CAPACITY;
+  if (!aligned16({kv.k, kv.v})) return RC_E_UNSUPPORTED;
+  const KvGeom k = geom_of(kv);
+  *g = {kv.n_blocks * kv.block_size, kv.block_size, kv.n_kv_heads, kv.head_dim, k.div_mul, k.div_shift};
+  return RC_OK;
+}
+
+rc_status rc_batch_map(const rc_batch_map_args* a, void* stream) {
+  if (!a || a->n_seq < 1 || a->max_rows < 0 || !a->n_cached || !a->n_new || !a->block_table || a->max_blocks_per_seq < 1 ||
+      a->block_size < 1 || a->n_blocks < 1 || a->n_free < 0 || a->n_docs < 0 || !a->row_start)
+    return RC_E_INVALID_ARG;
+  if (a->n_free > 0 && !a->free_blocks) return RC_E_INVALID_ARG;
+  if (a->n_docs > 0 && (!a->doc_start || !a->doc_first)) return RC_E_INVALID_ARG;
+  // every workgroup reads the lengths, one of them writes these: they have to be apart
+  if (a->kv_len && (a->kv_len == a->n_cached || a->kv_len == a->n_new)) return RC_E_INVALID_ARG;
+  if (a->counts && a->free_first >= a->counts && a->free_first < a->counts + 3) return RC_E_INVALID_ARG;
+  if (a->n_seq > 65536 || (long)a->n_blocks * a->block_size > INT_MAX || (long)a->max_blocks_per_seq * a->block_size > INT_MAX)
+    return RC_E_CAPACITY;
+  RC_HIP(launch_batch_map(*a, reinterpret_cast<hipStream_t>(stream)));
+  return RC_OK;
+}
+
+rc_status rc_norm_rotary_rows(const void* qkv, int32_t qkv_dtype, int64_t qkv_stride, int32_t n, const int32_t* n_live,
+                              int32_t n_q_heads, const void* g_q, const void* g_k, float eps, const rc_rotary* rotary, const int32_t* pos,
+                              const int32_t* slot, const rc_kv_layer* dst, void* k_pre, void* q_out, void* stream) {
+  RC_TRY(check_kv_layer(dst));
+  RotaryArg rot;
+  RC_TRY(rotary_arg(rotary, dst->head_dim, &rot));
+  if (!qkv || !pos || !slot || !q_out || n < 0 || n_q_heads < 1 || n_q_heads % dst->n_kv_heads || !(eps >= 0.f)) return RC_E_INVALID_ARG;
+  if (qkv_dtype != RC_F32 && qkv_dtype != RC_BF16) return RC_E_INVALID_ARG;
+  if (qkv_stride < (int64_t)(n_q_heads + 2 * (int64_t)dst->n_kv_heads) * dst->head_dim) return RC_E_INVALID_ARG;
+  if (qkv_stride % 4 || !aligned16({qkv, g_q, g_k, k_pre, q_out})) return RC_E_UNSUPPORTED;
+  NormRotaryArgs a = {qkv, (long)qkv_stride, n, n_q_heads, n_live, g_q, g_k, eps, pos, slot, {}, dst->k, dst->v, k_pre, q_out};
+  RC_TRY(slot_geom_of(*dst, &a.g));
+  if (n == 0) return RC_OK;
+  RC_HIP(launch_norm_rotary(a, rot, qkv_dtype == RC_BF16, dst->dtype == RC_BF16, reinterpret_cast<hipStream_t>(stream)));
+  return RC_OK;
+}
+
+rc_status rc_rotary_move(const rc_kv_layer* src, const int32_t* src_slot, const rc_kv_layer* dst, const int32_t* dst_slot, int32_t n,
+                         const int32_t* n_live, const rc_rotary* rotary, const int32_t* new_pos, const int32_t* old_pos, void* stream) {
+  RC_TRY(check_kv_layer(src));
+  RC_TRY(check_kv_layer(dst));
+  if (src->n_kv_heads != dst->n_kv_heads || src->head_dim != dst->head_dim || src->dtype != dst->dtype) return RC_E_INVALID_ARG;
+  RotaryArg rot;
+  RC_TRY(rotary_arg(rotary, dst->head_dim, &rot));
+  if (!src_slot || !dst_slot || !new_pos || n < 0) return RC_E_INVALID_ARG;
+  RotaryMoveArgs a = {src->k, src->v, dst->k, dst->v, {}, {}, src_slot, dst_slot, new_pos, old_pos, n_live, n};
+  RC_TRY(slot_geom_of(*src, &a.gs));
+  RC_TRY(slot_geom_of(*dst, &a.gd));
+  if (n == 0) return RC_OK;
+  RC_HIP(launch_rotary_move(a, rot, src->dtype == RC_BF16, reinterpret_cast<hipStream_t>(stream)));
+  return RC_OK;
+}
+
+static rc_status masked_attention_args(const rc_masked_attention_args* d, int32_t n_q_heads, const rc_kv_layer* cache, MaskedAttnArgs* a) {
+  RC_TRY(check_kv_layer(cache));
+  if (!d || d->n_seq < 1 || d->n_rows < 0 || d->max_rows_per_seq < 1 || d->max_len < 1 || !d->row_start || !d->row_pos) return RC_E_INVALID_ARG;
+  if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads) return RC_E_INVALID_ARG;
+  if (!(d->scale >= 0.f) || !(d->cap >= 0.f) || std::isinf(d->scale) || std::isinf(d->cap)) return RC_E_INVALID_ARG;
+  if (n_q_heads / cache->n_kv_heads > 128 || !aligned16({cache->k, cache->v})) return RC_E_UNSUPPORTED;
+  if (d->n_seq > 65536 || (!d->seq && d->n_seq > cache->n_seq)) return RC_E_CAPACITY;
+  if ((long)d->max_len > (long)cache->max_blocks_per_seq * cache->block_size) return RC_E_CAPACITY;
+  if ((long)cache->n_blocks * cache->block_size * cache->n_kv_heads > INT_MAX) return RC_E_CAPACITY;
+  *a = {};
+  a->k_pool = cache->k;
+  a->v_pool = cache->v;
+  a->g = geom_of(*cache);
+  a->n_table_rows = cache->n_seq;
+  a->n_q_heads = n_q_heads;
+  a->n_seq = d->n_seq;
+  a->n_rows = d->n_rows;
+  a->max_rows_per_seq = std::min(d->max_rows_per_seq, std::max(d->n_rows, 1));
+  a->max_len = d->max_len;
+  a->row_start = d->row_start;
+  a->row_pos = d->row_pos;
+  a->row_lo = d->row_lo;
+  a->row_hi = d->row_hi;
+  a->seq = d->seq;
+  a->slopes = d->slopes;
+  a->scale = d->scale > 0.f ? d->scale : 1.0f / std::sqrt((float)cache->head_dim);
+  a->cap = d->cap;
+  return RC_OK;
+}
+
+size_t rc_masked_attention_workspace_bytes(const rc_masked_attention_args* args, int32_t n_q_heads, const rc_kv_layer* cache) {
+  MaskedAttnArgs a;
+  if (masked_attention_args(args, n_q_heads, cache, &a) != RC_OK) return 0;
+  return align_up(sizeof(float) * masked_attention_partial_floats(a, cache->dtype == RC_BF16));
+}
+
+rc_status rc_masked_attention(const void* q, const rc_masked_attention_args* args, int32_t n_q_heads, const rc_kv_layer* cache, void* out,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  MaskedAttnArgs a;
+  RC_TRY(masked_attention_args(args, n_q_heads, cache, &a));
+  if (!q || !out) return RC_E_INVALID_ARG;
+  if (!aligned16({q, out})) return RC_E_UNSUPPORTED;
+  const bool is_bf16 = cache->dtype == RC_BF16;
+  if (workspace && ((reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+                    sizeof(float) * masked_attention_partial_floats(a, is_bf16) > workspace_bytes))
+    return RC_E_WORKSPACE;
+  if (a.n_rows == 0) return RC_OK;
+  a.q = q;
+  a.out = out;
+  RC_HIP(launch_masked_attention(a, is_bf16, reinterpret_cast<float*>(workspace), reinterpret_cast<hipStream_t>(stream)));
   return RC_OK;
 }
 

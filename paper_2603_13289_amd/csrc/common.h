@@ -484,6 +484,52 @@ size_t mfma_loop_out_floats(int n_workgroups);
 double mfma_loop_flops(int n_workgroups, int iters);
 hipError_t launch_mfma_loop(float* out, int n_workgroups, int iters, hipStream_t st);
 
+// ------------------------------------------------------------------ ragged batches (batch_rows.hip, attention_masked.hip)
+// The rotation as kernels take it: turns[i] = freq[i] / 2 pi, so that a position's angle is reduced by dropping whole turns.
+struct RotaryArg { int layout, rotary_dim; float amplitude; double turns[RC_ROTARY_MAX_PAIRS]; };
+
+// pool rows by slot: (slot, head) -> element offset; slots outside the pool are the caller's to skip
+struct SlotGeom { int rows, block_size, n_kv_heads, head_dim; unsigned div_mul; int div_shift; };
+__device__ inline size_t slot_offset(const SlotGeom& g, int slot, int head) {
+  const int blk = (int)(((unsigned long long)(2u * (unsigned)slot) * g.div_mul) >> 32 >> g.div_shift);   // block_of
+  return (((size_t)blk * g.n_kv_heads + head) * g.block_size + (slot - blk * g.block_size)) * (size_t)g.head_dim;
+}
+
+hipError_t launch_batch_map(const rc_batch_map_args& a, hipStream_t st);
+struct NormRotaryArgs {
+  const void* qkv;
+  long stride;
+  int n, n_q_heads;
+  const int* n_live;
+  const void *g_q, *g_k;
+  float eps;
+  const int *pos, *slot;
+  SlotGeom g;
+  void *k_pool, *v_pool, *k_pre, *q_out;
+};
+hipError_t launch_norm_rotary(const NormRotaryArgs& a, const RotaryArg& rot, bool qkv_bf16, bool pool_bf16, hipStream_t st);
+struct RotaryMoveArgs {
+  const void *k_src, *v_src;
+  void *k_dst, *v_dst;
+  SlotGeom gs, gd;
+  const int *src_slot, *dst_slot, *new_pos, *old_pos, *n_live;
+  int n;
+};
+hipError_t launch_rotary_move(const RotaryMoveArgs& a, const RotaryArg& rot, bool pool_bf16, hipStream_t st);
+
+struct MaskedAttnArgs {
+  const void *q, *k_pool, *v_pool;
+  void* out;
+  KvGeom g;
+  int n_table_rows;   // of the block table
+  int n_q_heads, n_seq, n_rows, max_rows_per_seq, max_len;
+  const int *row_start, *row_pos, *row_lo, *row_hi, *seq;
+  const float* slopes;
+  float scale, cap;
+};
+size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16);
+hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float* part, hipStream_t st);
+
 template <typename T>
 hipError_t launch_scatter_rows(const T* k_rows, const T* v_rows, const int* pos, int n, T* k_pool,
                                T* v_pool, KvGeom g, int seq, hipStream_t st);
