@@ -1468,7 +1468,7 @@ static rc_status masked_attention_args(const rc_masked_attention_args* d, int32_
   if (!(d->scale >= 0.f) || !(d->cap >= 0.f) || std::isinf(d->scale) || std::isinf(d->cap)) return RC_E_INVALID_ARG;
   if (n_q_heads / cache->n_kv_heads > 128 || !aligned16({cache->k, cache->v})) return RC_E_UNSUPPORTED;
   if (d->n_seq > 65536 || (!d->seq && d->n_seq > cache->n_seq)) return RC_E_CAPACITY;
-  if ((long)d->max_len > (long)cache->max_blocks_per_seq * cache->block_size) return RC_E_CAPACITY;
+  if ((long)d->max_len > (long)cache->max_blocks_per_seq * cache->block_size || d->max_len > (1 << 30)) return RC_E_CAPACITY;
   if ((long)cache->n_blocks * cache->block_size * cache->n_kv_heads > INT_MAX) return RC_E_CAPACITY;
   *a = {};
   a->k_pool = cache->k;

@@ -1,70 +1,655 @@
 // Grouped-query attention of a ragged batch: scores capped by a tanh or biased by distance, a key range for every row.
+//
+// A row and head of a key head's group is a column of the products.  Per 32 or 64 keys, on 32x32x16 matrix instructions,
+//   S^T[key][column] = K[key][:] . Q[column][:]     A: K rows from LDS, B: Q in registers
+//   O^T[d][column]  += V^T[d][key] P[key][column]   A: V rows from LDS, transposed by the read; B: P, S^T's registers as they stand
+// so that a column's scores lie in two lanes (c, c + 32) and its softmax takes one exchange between them.  P's element order is a
+// permutation of the keys inside a group of 16 (a lane of half h has keys 4h .. 4h + 3 and 8 + 4h .. 8 + 4h + 3); the transposing read
+// takes four keys at a time, so it follows that order for nothing.
+//
+// In LDS a row is 256 bytes; its 16-byte pieces change places by the key: K's piece c is at c ^ (key & 15), which lets eight (sixteen) lanes that
+// fetch one piece of consecutive keys meet every bank once, V's at c ^ 4 (key & 3), which does so for the four keys of a transposing read.
+#include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "common.h"
 
 namespace rc {
 
-// One wavefront per (row, head): 64 keys at a time, a lane a key for the scores, two elements of the head a lane for the values.
-template <typename T>
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
+typedef __attribute__((__vector_size__(8 * sizeof(float)))) float f32x8;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+
+static constexpr int DH = 128;
+static constexpr int BKV = 64;            // keys per tile of the tile kernel
+static constexpr int TILE_COLS = 128;     // columns of a tile: four wavefronts, 32 each
+static constexpr int ROW_COLS = 32;       // columns of the few-row kernel
+static constexpr int ROW_KEYS = 32;       // keys a wavefront of it takes at a time
+static constexpr int PROW = DH + 4;       // floats between the columns of a partial result
+static constexpr float kRescaleSlack = 8.f;   // log2 units the running maximum may lead the reference exponent
+static constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ inline float pair_max(float x) {   // over lanes l, l ^ 32
+  const unsigned u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Rows r0 .. r1 - 1 of a sequence, whatever the device says inside [0, n_rows].
+struct SeqRows { int r0, r1, table_row; };
+__device__ inline SeqRows rows_of_seq(const MaskedAttnArgs& a, int s) {
+  SeqRows q;
+  q.r0 = min(max(a.row_start[s], 0), a.n_rows);
+  q.r1 = min(max(a.row_start[s + 1], q.r0), min(a.n_rows, q.r0 + a.max_rows_per_seq));
+  q.table_row = a.seq ? min(max(a.seq[s], 0), a.n_table_rows - 1) : s;
+  return q;
+}
+// Keys that a row sees; (INT_MAX, -1) where it sees none.
+struct Range { int lo, hi; };
+__device__ inline Range range_of_row(const MaskedAttnArgs& a, int row) {
+  const int lo = max(a.row_lo ? a.row_lo[row] : 0, 0), hi = min(a.row_hi ? a.row_hi[row] : a.row_pos[row], a.max_len - 1);
+  return lo <= hi ? Range{lo, hi} : Range{INT_MAX, -1};
+}
+// The last i with start(i) <= x, start ascending; start(0) <= x.  64 candidates a step.
+template <typename F>
+__device__ inline int last_at_or_before(int n, int x, F start) {
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  while (true) {
+    const int step = (n - base + 63) / 64;
+    const int i = base + lane * step;
+    const unsigned long long at = __ballot(i < n && start(min(i, n - 1)) <= x);
+    base += (at ? 63 - __clzll((long long)at) : 0) * step;
+    base = __builtin_amdgcn_readfirstlane(base);
+    if (step <= 1) return base;
+    n = min(n, base + step);
+  }
+}
+
+// Scores in units of log2: what a weight is 2 to the power of.
+template <bool CAP, bool BIAS>
+struct Score {
+  float scale, twice, cap, slope, from;   // from: key offset of the lane's element 0 minus the row's position
+  // the cap's tanh(x / cap) = 1 - 2 / (exp(2 x / cap) + 1): an error of 2^-23 of the cap, a weight's relative error of as much times the cap, where
+  // the weight is rounded to 2^-8 in any case
+  __device__ Score(const MaskedAttnArgs& a) : scale(a.scale * kLog2e), twice(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap(a.cap * kLog2e), slope(0.f), from(0.f) {}
+  __device__ float operator()(float dot, float offset) const {
+    float x;
+    if constexpr (CAP) x = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * twice) + 1.f), cap);
+    else x = dot * scale;
+    if constexpr (BIAS) x = fmaf(-slope, fabsf(from + offset), x);
+    return x;
+  }
+};
+
+// 16 bytes of a value row: halves that are not finite become zeros (they would turn a weight of 0 into NaN); true if there was one.
+__device__ inline bool only_finite(uint4& v) {
+  bool bad = false;
+  uint32_t* const w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((w[i] & 0x7f80u) == 0x7f80u) { w[i] &= 0xffff0000u; bad = true; }
+    if ((w[i] & 0x7f800000u) == 0x7f800000u) { w[i] &= 0xffffu; bad = true; }
+  }
+  return bad;
+}
+// What such values of keys key0 .. key0 + n - 1 add to the columns that see them: an infinity or NaN, whatever the weight.
+__device__ __forceinline__ void add_not_finite(const bf16* v_pool, KvGeom g, int seq, int kvh, int key0, int n, Range r, f32x16 (&acc_o)[4]) {
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll 1
+  for (int j = 0; j < n; ++j) {
+    const int key = key0 + j;
+    if (!__any(r.lo <= key && key <= r.hi)) continue;
+    const bf16* const v = v_pool + kv_row_offset(g, seq, key, kvh) + 4 * half;
+    const bool sees = r.lo <= key && key <= r.hi;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = to_f32(v[32 * db + 8 * (e >> 2) + (e & 3)]);
+        if (sees && !(fabsf(x) < INFINITY)) acc_o[db][e] += x;
+      }
+  }
+}
+
+// The running softmax of a column over 16 B keys (B blocks of 32 scores, in two lanes): scores become weights.
+// The reference exponent follows the maximum lazily: the sums are rescaled only when a column's maximum has grown by more than
+// kRescaleSlack since the last time, so weights stay below 2^kRescaleSlack instead of 1; any reference gives the same quotient.
+template <int B>
+__device__ __forceinline__ void online_softmax(f32x16 (&s)[B], float& m_run, float& l_run, f32x16 (&acc_o)[4], bf16x8 (&p)[2 * B]) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int b = 0; b < B; ++b)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
+  mx = pair_max(mx);
+  const float m_new = fmaxf(m_run, mx);
+  if (__any(m_new > m_run + kRescaleSlack)) {
+    const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
+    l_run *= corr;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc_o[i][e] *= corr;
+    m_run = m_new;
+  }
+  const float m_use = m_run == -INFINITY ? 0.f : m_run;
+  float sum = 0.f;
+#pragma unroll
+  for (int u = 0; u < 2 * B; ++u) {
+    f32x8 w;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      w[j] = __builtin_amdgcn_exp2f(s[u >> 1][8 * (u & 1) + j] - m_use);
+      sum += w[j];
+    }
+    p[u] = __builtin_convertvector(w, bf16x8);   // rounded for the product; the sum takes them as they are
+  }
+  l_run += sum;
+}
+
+__device__ inline bf16x8 k_fragment(const unsigned char* k, int key, int piece) {
+  return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k + key * 256 + 16 * (piece ^ (key & 15))));
+}
+// V^T operand of keys 16 t .. 16 t + 15 and d = 32 db .. 32 db + 31
+__device__ inline bf16x8 v_fragment(const unsigned char* v, int lane, int t, int db) {
+  const int key = 16 * t + 4 * (lane >> 5) + ((lane >> 2) & 3);
+  const int byte = 64 * db + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+  auto at = [&](int k) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) s16x4*)(v + k * 256 + (byte ^ (64 * (k & 3)))));
+  };
+  const s16x4 a = at(key), b = at(key + 8);
+  typedef __attribute__((__vector_size__(8 * sizeof(short)))) short s16x8;
+  return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// how a batch's key ranges are cut
+struct MaskedSplit { int n_chunks, chunk; };   // chunk: keys
+
+__device__ inline uint2 pack4(float a, float b, float c, float d) {
+  return make_uint2((uint32_t)f32_to_bf16(a).v | ((uint32_t)f32_to_bf16(b).v << 16), (uint32_t)f32_to_bf16(c).v | ((uint32_t)f32_to_bf16(d).v << 16));
+}
+
+// ------------------------------------------------------------------ tiles of 128 columns
+// Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
+// over the sequences (ceil(n / R) <= floor((a + n) / R) - floor(a / R) + 1).
+template <bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2)
+masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, float* __restrict__ part_o, float2* __restrict__ part_ml) {
+  __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][BKV * 256];   // [buffer][K, V]
+  __shared__ int bad_v[2][4];
+  const int kvh = (int)blockIdx.x % a.g.n_kv_heads;
+  const int item = (int)blockIdx.x / a.g.n_kv_heads;
+  const int slot = n_slots - 1 - item / sp.n_chunks, chunk = item % sp.n_chunks;   // late rows see the most keys: they go first
+  const int G = a.n_q_heads / a.g.n_kv_heads;
+  const int s = last_at_or_before(a.n_seq, slot, [&](int i) { return min(max(a.row_start[i], 0), a.n_rows) / rows_per_tile + i; });
+  const SeqRows sq = rows_of_seq(a, s);
+  const int first = sq.r0 + (slot - (sq.r0 / rows_per_tile + s)) * rows_per_tile;
+  const int n_valid = min(rows_per_tile, sq.r1 - first);
+  if (n_valid <= 0 || first < sq.r0) return;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, half = lane >> 5;
+  int lo_min = INT_MAX, lo_max = 0, hi_min = INT_MAX, hi_max = -1;
+  for (int i = lane; i < n_valid; i += 64) {
+    const Range r = range_of_row(a, first + i);
+    lo_min = min(lo_min, r.lo); lo_max = max(lo_max, r.lo); hi_min = min(hi_min, r.hi); hi_max = max(hi_max, r.hi);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    lo_min = min(lo_min, __shfl_xor(lo_min, o, 64)); lo_max = max(lo_max, __shfl_xor(lo_max, o, 64));
+    hi_min = min(hi_min, __shfl_xor(hi_min, o, 64)); hi_max = max(hi_max, __shfl_xor(hi_max, o, 64));
+  }
+  lo_min = __builtin_amdgcn_readfirstlane(lo_min); lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+  hi_min = __builtin_amdgcn_readfirstlane(hi_min); hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+  const bool is_split = sp.n_chunks > 1;
+  const int key_end = is_split ? min(hi_max + 1, (chunk + 1) * sp.chunk) : hi_max + 1;   // chunk sizes are whole tiles, chunks * size < 2^31 (host)
+  const int t_begin = hi_max < 0 ? 0 : max(lo_min, chunk * sp.chunk) / BKV, t_end = (key_end + BKV - 1) / BKV;
+  if (t_begin >= t_end && is_split) return;
+
+  const int col = wave * 32 + ql, my = col / G;
+  const bool live = col < rows_per_tile * G && my < n_valid;
+  const int row = first + min(my, n_valid - 1), head = kvh * G + col % G;
+  const Range mine = range_of_row(a, row);
+  const unsigned seen = mine.hi < 0 ? 0u : (unsigned)(mine.hi - mine.lo) + 1u;
+
+  bf16x8 qf[8];
+  {
+    const bf16* const q = reinterpret_cast<const bf16*>(a.q) + ((size_t)row * a.n_q_heads + head) * DH + 8 * half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q + 16 * i));
+  }
+  Score<CAP, BIAS> score(a);
+  if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
+  const int pos = a.row_pos[row];
+
+  // A lane looks up the pool row of one key of a tile, two tiles ahead; a thread loads 16 bytes of four rows.
+  const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
+  struct Asked { int block, slot; };
+  auto ask = [&](int t) __attribute__((always_inline)) -> Asked {
+    const int key = min(t * BKV + lane, a.max_len - 1), at = block_of(a.g, key);
+    return {table[min(at, a.g.max_blocks - 1)], key - at * a.g.block_size};
+  };
+  uint4 rk[4], rv[4];
+  auto fetch = [&](Asked q) __attribute__((always_inline)) {
+    const unsigned pool_row = (unsigned)(min(max(q.block, 0), a.g.n_blocks - 1) * a.g.n_kv_heads + kvh) * (unsigned)a.g.block_size + q.slot;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const size_t off = (size_t)(unsigned)__shfl((int)pool_row, (tid >> 4) + 16 * i, 64) * 256 + (tid & 15) * 16;
+      rk[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.k_pool) + off);
+      rv[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.v_pool) + off);
+    }
+  };
+  auto whole = [&](int t) { return t * BKV >= lo_max && t * BKV + BKV - 1 <= hi_min; };   // every row of the tile sees all of its keys
+  auto stage = [&](int t, int buf) __attribute__((always_inline)) {
+    bool bad = false;
+    if (!whole(t)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bad |= only_finite(rv[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = (tid >> 4) + 16 * i, piece = tid & 15;
+      *reinterpret_cast<uint4*>(&lds[buf][0][key * 256 + 16 * (piece ^ (key & 15))]) = rk[i];
+      *reinterpret_cast<uint4*>(&lds[buf][1][key * 256 + 16 * (piece ^ (4 * (key & 3)))]) = rv[i];
+    }
+    const bool any_bad = __any(bad);
+    if (lane == 0) bad_v[buf][wave] = any_bad;
+  };
+
+  f32x16 acc_o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  if (t_begin < t_end) {
+    fetch(ask(t_begin));
+    const Asked second = ask(t_begin + 1);
+    stage(t_begin, 0);
+    fetch(second);
+  }
+  __syncthreads();
+  for (int t = t_begin; t < t_end; ++t) {
+    const int buf = (t - t_begin) & 1;
+    const unsigned char* const k = lds[buf][0];
+    const unsigned char* const v = lds[buf][1];
+    const Asked next2 = ask(t + 2);
+    f32x16 acc_s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc_s[b][e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        acc_s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(k, 32 * b + ql, 2 * i + half), qf[i], acc_s[b], 0, 0, 0);
+    if (t + 1 < t_end) stage(t + 1, buf ^ 1);
+    if (t + 2 < t_end) fetch(next2);
+    if constexpr (BIAS) score.from = (float)(t * BKV + 4 * half - pos);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc_s[b][e] = score(acc_s[b][e], (float)(32 * b + 8 * (e >> 2) + (e & 3)));
+    if (!whole(t)) {
+      const int key0 = t * BKV + 4 * half - mine.lo;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((unsigned)(key0 + 32 * b + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[b][e] = -INFINITY;
+    }
+    bf16x8 p[4];
+    online_softmax<2>(acc_s, m_run, l_run, acc_o, p);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+        acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(v, lane, u, db), p[u], acc_o[db], 0, 0, 0);
+    if (!whole(t) && (bad_v[buf][0] | bad_v[buf][1] | bad_v[buf][2] | bad_v[buf][3]))
+      add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, t * BKV, min(BKV, a.max_len - t * BKV), mine, acc_o);
+    __syncthreads();   // tile t consumed, tile t + 1 staged
+  }
+
+  const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+  if (!live) return;
+  if (is_split) {
+    const size_t at = ((size_t)(slot * (long)sp.n_chunks + chunk) * a.g.n_kv_heads + kvh) * TILE_COLS + col;
+    if (half == 0) part_ml[at] = make_float2(m_run, l_tot);
+    float* const o = part_o + at * PROW + 4 * half;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<float4*>(o + 32 * db + 2 * e) = make_float4(acc_o[db][e], acc_o[db][e + 1], acc_o[db][e + 2], acc_o[db][e + 3]);
+    return;
+  }
+  const float inv = seen ? 1.0f / l_tot : 0.f;
+  bf16* const o = reinterpret_cast<bf16*>(a.out) + ((size_t)row * a.n_q_heads + head) * DH + 4 * half;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<uint2*>(o + 32 * db + 2 * e) = pack4(acc_o[db][e] * inv, acc_o[db][e + 1] * inv, acc_o[db][e + 2] * inv, acc_o[db][e + 3] * inv);
+}
+
+// ------------------------------------------------------------------ few rows a sequence: at most 32 columns
+// A workgroup takes a sequence's columns and a range of keys; its wavefronts take every fourth block of 32 keys of the range with a softmax of
+// their own and share nothing before the end.
+static constexpr int kRowWaveBytes = ROW_COLS * PROW * 4;   // a wavefront's K and V (16 KB), at the end its sums
+template <bool CAP, bool BIAS>
+__global__ void __launch_bounds__(256, 2)
+masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ part_o, float2* __restrict__ part_ml) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds_rows[];
+  __shared__ float2 ml[4][ROW_COLS];
+  const int kvh = (int)blockIdx.x % a.g.n_kv_heads;
+  const int item = (int)blockIdx.x / a.g.n_kv_heads;
+  const int s = item / sp.n_chunks, chunk = item - s * sp.n_chunks;
+  const int G = a.n_q_heads / a.g.n_kv_heads;
+  const SeqRows sq = rows_of_seq(a, s);
+  const int n_cols = (sq.r1 - sq.r0) * G;   // at most 32 (host)
+  if (n_cols <= 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+  const int row = sq.r0 + min(col, n_cols - 1) / G, head = kvh * G + min(col, n_cols - 1) % G;
+  const Range mine = range_of_row(a, row);
+  const unsigned seen = mine.hi < 0 ? 0u : (unsigned)(mine.hi - mine.lo) + 1u;
+  int lo_min = mine.lo, lo_max = mine.lo, hi_min = mine.hi, hi_max = mine.hi;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    lo_min = min(lo_min, __shfl_xor(lo_min, o, 64)); lo_max = max(lo_max, __shfl_xor(lo_max, o, 64));
+    hi_min = min(hi_min, __shfl_xor(hi_min, o, 64)); hi_max = max(hi_max, __shfl_xor(hi_max, o, 64));
+  }
+  lo_min = __builtin_amdgcn_readfirstlane(lo_min); lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+  hi_min = __builtin_amdgcn_readfirstlane(hi_min); hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+  const bool is_split = sp.n_chunks > 1;
+  const int key_end = is_split ? min(hi_max + 1, (chunk + 1) * sp.chunk) : hi_max + 1;
+  const int b_begin = hi_max < 0 ? 0 : max(lo_min, chunk * sp.chunk) / ROW_KEYS, b_end = (key_end + ROW_KEYS - 1) / ROW_KEYS;
+  if (b_begin >= b_end && is_split) return;
+
+  bf16x8 qf[8];
+  {
+    const bf16* const q = reinterpret_cast<const bf16*>(a.q) + ((size_t)row * a.n_q_heads + head) * DH + 8 * half;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q + 16 * i));
+  }
+  Score<CAP, BIAS> score(a);
+  if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
+  const int pos = a.row_pos[row];
+
+  const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
+  struct Asked { int block, slot; };
+  auto ask = [&](int b) __attribute__((always_inline)) -> Asked {
+    const int key = min(min(b, b_end - 1) * ROW_KEYS + col, a.max_len - 1), at = block_of(a.g, key);
+    return {table[min(at, a.g.max_blocks - 1)], key - at * a.g.block_size};
+  };
+  uint4 rk[8], rv[8];
+  auto fetch = [&](Asked q) __attribute__((always_inline)) {
+    const unsigned pool_row = (unsigned)(min(max(q.block, 0), a.g.n_blocks - 1) * a.g.n_kv_heads + kvh) * (unsigned)a.g.block_size + q.slot;
+    size_t off[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) off[i] = (size_t)(unsigned)__shfl((int)pool_row, 4 * i + (lane >> 4), 64) * 256 + (lane & 15) * 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rk[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.k_pool) + off[i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rv[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.v_pool) + off[i]);
+  };
+
+  f32x16 acc_o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  unsigned char* const k = lds_rows + wave * kRowWaveBytes;
+  unsigned char* const v = k + ROW_KEYS * 256;
+  int b = b_begin + wave;
+  if (b < b_end) {
+    Asked next = ask(b);
+    fetch(next);
+    next = ask(b + 4);
+    for (; b < b_end; b += 4) {
+      const bool whole = b * ROW_KEYS >= lo_max && b * ROW_KEYS + ROW_KEYS - 1 <= hi_min;
+      bool bad = false;
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bad |= only_finite(rv[i]);
+      }
+      // this wavefront's own memory, and its LDS accesses stay in order: no barrier
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int key = 4 * i + (lane >> 4), piece = lane & 15;
+        *reinterpret_cast<uint4*>(k + key * 256 + 16 * (piece ^ (key & 15))) = rk[i];
+        *reinterpret_cast<uint4*>(v + key * 256 + 16 * (piece ^ (4 * (key & 3)))) = rv[i];
+      }
+      asm volatile("" ::: "memory");
+      if (b + 4 < b_end) {
+        fetch(next);
+        next = ask(b + 8);
+      }
+      f32x16 acc_s[1];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc_s[0][e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        acc_s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(k, col, 2 * i + half), qf[i], acc_s[0], 0, 0, 0);
+      if constexpr (BIAS) score.from = (float)(b * ROW_KEYS + 4 * half - pos);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc_s[0][e] = score(acc_s[0][e], (float)(8 * (e >> 2) + (e & 3)));
+      if (!whole) {
+        const int key0 = b * ROW_KEYS + 4 * half - mine.lo;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if ((unsigned)(key0 + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[0][e] = -INFINITY;
+      }
+      bf16x8 p[2];
+      online_softmax<1>(acc_s, m_run, l_run, acc_o, p);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+          acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(v, lane, u, db), p[u], acc_o[db], 0, 0, 0);
+      if (__any(bad))
+        add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, b * ROW_KEYS, min(ROW_KEYS, a.max_len - b * ROW_KEYS), mine, acc_o);
+      asm volatile("" ::: "memory");
+    }
+  }
+
+  // the four wavefronts' sums, in their order
+  const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
+  if (half == 0) ml[wave][col] = make_float2(m_run, l_tot);
+  __syncthreads();
+  float m_all = ml[0][col].x;
+#pragma unroll
+  for (int w = 1; w < 4; ++w) m_all = fmaxf(m_all, ml[w][col].x);
+  const float mine_by = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
+  float* const sums = reinterpret_cast<float*>(k);
+  if (col < n_cols) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4)
+        *reinterpret_cast<float4*>(sums + col * PROW + 32 * db + 2 * e + 4 * half) =
+            m_run == -INFINITY ? make_float4(0.f, 0.f, 0.f, 0.f)
+                               : make_float4(acc_o[db][e] * mine_by, acc_o[db][e + 1] * mine_by, acc_o[db][e + 2] * mine_by, acc_o[db][e + 3] * mine_by);
+  }
+  __syncthreads();
+  for (int i = tid; i < n_cols * (DH / 4); i += 256) {
+    const int c = i / (DH / 4), d = (i - c * (DH / 4)) * 4;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = ml[0][c].x, l = 0.f;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, ml[w][c].x);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float4 x = *reinterpret_cast<const float4*>(lds_rows + w * kRowWaveBytes + (c * PROW + d) * 4);
+      o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+      l += ml[w][c].x == -INFINITY ? 0.f : ml[w][c].y * __builtin_amdgcn_exp2f(ml[w][c].x - m);
+    }
+    if (is_split) {
+      const size_t at = ((size_t)item * a.g.n_kv_heads + kvh) * ROW_COLS + c;
+      if (d == 0) part_ml[at] = make_float2(m, l);
+      *reinterpret_cast<float4*>(part_o + at * PROW + d) = o;
+    } else {
+      const int r = sq.r0 + c / G, h = kvh * G + c % G;
+      const Range range = range_of_row(a, r);
+      const float inv = range.hi < 0 ? 0.f : 1.0f / l;
+      *reinterpret_cast<uint2*>(reinterpret_cast<bf16*>(a.out) + ((size_t)r * a.n_q_heads + h) * DH + d) = pack4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ merge of the chunks
+// A wavefront per (row, head), 32 lanes with four elements each of every other chunk.  A chunk left a result for a column
+// exactly if the tile's range reaches into it, which it does where the row's own range does.
 __global__ void __launch_bounds__(256)
-masked_attn_row_kernel(MaskedAttnArgs a) {
+masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int cols, int rows_per_tile, const float* __restrict__ part_o,
+                         const float2* __restrict__ part_ml) {
+  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int row = (int)(item / a.n_q_heads), head = (int)(item - (long)row * a.n_q_heads);
+  if (row >= a.n_rows) return;
+  const int lane = threadIdx.x & 63, d = (lane & 31) * 4, odd = lane >> 5;
+  const int G = a.n_q_heads / a.g.n_kv_heads, kvh = head / G;
+  const int s = last_at_or_before(a.n_seq, row, [&](int i) { return min(max(a.row_start[i], 0), a.n_rows); });
+  const SeqRows sq = rows_of_seq(a, s);
+  if (row < sq.r0 || row >= sq.r1) return;
+  const Range r = range_of_row(a, row);
+  bf16* const out = reinterpret_cast<bf16*>(a.out) + ((size_t)row * a.n_q_heads + head) * DH + d;
+  if (r.hi < 0) {
+    if (!odd) *reinterpret_cast<uint2*>(out) = make_uint2(0u, 0u);
+    return;
+  }
+  const int in_seq = row - sq.r0;
+  const long slot = cols == ROW_COLS ? s : sq.r0 / rows_per_tile + s + in_seq / rows_per_tile;
+  const int col = (cols == ROW_COLS ? in_seq : in_seq % rows_per_tile) * G + head - kvh * G;
+  const int c0 = r.lo / sp.chunk, c1 = r.hi / sp.chunk;
+  auto at = [&](int c) { return ((size_t)(slot * sp.n_chunks + c) * a.g.n_kv_heads + kvh) * cols + col; };
+  float m = -INFINITY;
+  for (int c = c0 + lane; c <= c1; c += 64) m = fmaxf(m, part_ml[at(c)].x);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  float l = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c = c0 + odd; c <= c1; c += 2) {
+    const float2 x = part_ml[at(c)];
+    if (x.x == -INFINITY) continue;
+    const float w = __builtin_amdgcn_exp2f(x.x - m);
+    const float4 o = *reinterpret_cast<const float4*>(part_o + at(c) * PROW + d);
+    l += x.y * w;
+    acc.x += o.x * w; acc.y += o.y * w; acc.z += o.z * w; acc.w += o.w * w;
+  }
+  l += __shfl_xor(l, 32, 64);
+  acc.x += __shfl_xor(acc.x, 32, 64); acc.y += __shfl_xor(acc.y, 32, 64); acc.z += __shfl_xor(acc.z, 32, 64); acc.w += __shfl_xor(acc.w, 32, 64);
+  const float inv = 1.0f / l;
+  if (!odd) *reinterpret_cast<uint2*>(out) = pack4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+}
+
+// ------------------------------------------------------------------ float: one wavefront per (row, head)
+// 64 keys at a time, a lane a key for the scores, an element or two of the head a lane for the values.
+__global__ void __launch_bounds__(256)
+masked_attn_f32_kernel(MaskedAttnArgs a) {
   const int lane = threadIdx.x & 63;
   const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int row = (int)(item / a.n_q_heads), head = (int)(item - (long)row * a.n_q_heads);
   if (row >= a.n_rows) return;
-  int s = 0, e = a.n_seq;   // the last sequence that begins at or before the row
-  while (e - s > 1) {
-    const int m = (s + e) >> 1;
-    if (a.row_start[m] <= row) s = m; else e = m;
-  }
-  const int first = a.row_start[s];
-  if (row < first || row >= a.row_start[s + 1] || row - first >= a.max_rows_per_seq) return;
-  const int seq = a.seq ? min(max(a.seq[s], 0), a.n_table_rows - 1) : s;
+  const int s = last_at_or_before(a.n_seq, row, [&](int i) { return min(max(a.row_start[i], 0), a.n_rows); });
+  const SeqRows sq = rows_of_seq(a, s);
+  if (row < sq.r0 || row >= sq.r1) return;
   const int dh = a.g.head_dim, kvh = head / (a.n_q_heads / a.g.n_kv_heads);
   const int pos = a.row_pos[row];
-  const int lo = max(a.row_lo ? a.row_lo[row] : 0, 0), hi = min(a.row_hi ? a.row_hi[row] : pos, a.max_len - 1);
-  const T* const q = reinterpret_cast<const T*>(a.q) + ((size_t)row * a.n_q_heads + head) * dh;
+  const Range r = range_of_row(a, row);
+  const float* const q = reinterpret_cast<const float*>(a.q) + ((size_t)row * a.n_q_heads + head) * dh;
   const float slope = a.slopes ? a.slopes[head] : 0.f;
   float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (int k0 = lo; k0 <= hi; k0 += 64) {
-    const int key = min(k0 + lane, hi);
-    const size_t off = kv_row_offset(a.g, seq, key, kvh);
-    const T* const k = reinterpret_cast<const T*>(a.k_pool) + off;
+  for (long k0 = r.lo; k0 <= r.hi; k0 += 64) {
+    const int key = (int)min(k0 + lane, (long)r.hi);
+    const float* const k = reinterpret_cast<const float*>(a.k_pool) + kv_row_offset(a.g, sq.table_row, key, kvh);
     float x = 0.f;
-    for (int d = 0; d < dh; ++d) x += to_f32(q[d]) * to_f32(k[d]);
+    for (int d = 0; d < dh; ++d) x += q[d] * k[d];
     x *= a.scale;
     if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
     x -= slope * fabsf((float)(pos - key));
-    if (k0 + lane > hi) x = -INFINITY;
+    if (k0 + lane > r.hi) x = -INFINITY;
     float mx = x;
     for (int w = 32; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor(mx, w, 64));
     const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float corr = __expf(m - m_use), p = k0 + lane > hi ? 0.f : __expf(x - m_use);
+    const float corr = __expf(m - m_use), p = k0 + lane > r.hi ? 0.f : __expf(x - m_use);
     m = m_new;
     l = l * corr + p;
     o0 *= corr;
     o1 *= corr;
-    for (int j = 0; j < min(64, hi - k0 + 1); ++j) {
+    for (int j = 0; j < (int)min(64l, r.hi - k0 + 1); ++j) {
       const float w = __shfl(p, j, 64);
-      const T* const v = reinterpret_cast<const T*>(a.v_pool) + kv_row_offset(a.g, seq, k0 + j, kvh);
-      o0 += w * to_f32(v[lane]);
-      if (dh == 128) o1 += w * to_f32(v[lane + 64]);
+      const float* const v = reinterpret_cast<const float*>(a.v_pool) + kv_row_offset(a.g, sq.table_row, (int)k0 + j, kvh);
+      o0 += w * v[lane];
+      if (dh == 128) o1 += w * v[lane + 64];
     }
   }
   for (int w = 32; w > 0; w >>= 1) l += __shfl_xor(l, w, 64);
-  T* const out = reinterpret_cast<T*>(a.out) + ((size_t)row * a.n_q_heads + head) * dh;
-  const float inv = lo > hi ? 0.f : 1.f / l;
-  out[lane] = from_f32<T>(o0 * inv);
-  if (dh == 128) out[lane + 64] = from_f32<T>(o1 * inv);
+  float* const out = reinterpret_cast<float*>(a.out) + ((size_t)row * a.n_q_heads + head) * dh;
+  const float inv = r.hi < 0 ? 0.f : 1.f / l;
+  out[lane] = o0 * inv;
+  if (dh == 128) out[lane + 64] = o1 * inv;
 }
 
-size_t masked_attention_partial_floats(const MaskedAttnArgs&, bool) { return 0; }
+// ------------------------------------------------------------------ host
+// The few-row kernel serves sequences whose columns fit 32; the grid is then (sequence, chunk), else (tile, chunk).
+struct MaskedPlan { bool rows; int slots, rows_per_tile, cols; MaskedSplit split; };
+static MaskedPlan plan_masked(const MaskedAttnArgs& a) {
+  MaskedPlan p;
+  const int G = a.n_q_heads / a.g.n_kv_heads;
+  p.rows = (long)a.max_rows_per_seq * G <= ROW_COLS;
+  p.cols = p.rows ? ROW_COLS : TILE_COLS;
+  p.rows_per_tile = TILE_COLS / G;
+  p.slots = p.rows ? a.n_seq : a.n_rows / p.rows_per_tile + a.n_seq;
+  const long wgs = (long)p.slots * a.g.n_kv_heads;
+  const long unit = p.rows ? 4 * ROW_KEYS : BKV, least = p.rows ? 256 : 512, wanted = 1024;
+  long chunks = std::min(wanted / std::max(wgs, 1l), (a.max_len + least - 1) / least);
+  long chunk = chunks <= 1 ? 0 : ((a.max_len + chunks - 1) / chunks + unit - 1) / unit * unit;
+  p.split.n_chunks = chunk ? (int)((a.max_len + chunk - 1) / chunk) : 1;
+  p.split.chunk = (int)chunk;
+  return p;
+}
 
-hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float*, hipStream_t st) {
-  const unsigned grid = (unsigned)(((long)a.n_rows * a.n_q_heads + 3) / 4);
-  if (is_bf16) masked_attn_row_kernel<bf16><<<grid, 256, 0, st>>>(a);
-  else masked_attn_row_kernel<float><<<grid, 256, 0, st>>>(a);
+size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16) {
+  if (!is_bf16 || a.n_rows <= 0) return 0;
+  const MaskedPlan p = plan_masked(a);
+  if (p.split.n_chunks <= 1) return 0;
+  return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (PROW + 2);
+}
+
+template <bool CAP, bool BIAS>
+static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, float* part_o, float2* part_ml, hipStream_t st) {
+  const long grid = (long)p.slots * p.split.n_chunks * a.g.n_kv_heads;
+  if (grid > INT_MAX) return hipErrorInvalidValue;
+  if (p.rows) {
+    static std::atomic<unsigned long long> told{0};
+    const hipError_t e = allow_dynamic_lds((const void*)masked_attn_rows_kernel<CAP, BIAS>, 4 * kRowWaveBytes, told);
+    if (e != hipSuccess) return e;
+    masked_attn_rows_kernel<CAP, BIAS><<<(unsigned)grid, 256, 4 * kRowWaveBytes, st>>>(a, p.split, part_o, part_ml);
+  } else {
+    masked_attn_tile_kernel<CAP, BIAS><<<(unsigned)grid, 256, 0, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float* part, hipStream_t st) {
+  const unsigned per_row = (unsigned)(((long)a.n_rows * a.n_q_heads + 3) / 4);
+  if (!is_bf16) {
+    masked_attn_f32_kernel<<<per_row, 256, 0, st>>>(a);
+    return hipGetLastError();
+  }
+  MaskedPlan p = plan_masked(a);
+  if (!part) p.split = {1, 0};
+  float2* const part_ml = reinterpret_cast<float2*>(part + (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * PROW);
+  const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
+  const hipError_t e = cap ? (bias ? launch_bf16<true, true>(a, p, part, part_ml, st) : launch_bf16<true, false>(a, p, part, part_ml, st))
+                           : (bias ? launch_bf16<false, true>(a, p, part, part_ml, st) : launch_bf16<false, false>(a, p, part, part_ml, st));
+  if (e != hipSuccess || p.split.n_chunks <= 1) return e;
+  masked_attn_merge_kernel<<<per_row, 256, 0, st>>>(a, p.split, p.cols, p.rows_per_tile, part, part_ml);
   return hipGetLastError();
 }
 
