@@ -21,6 +21,7 @@ typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8;
 typedef __attribute__((__vector_size__(8 * sizeof(float)))) float f32x8;
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16;
 typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
+typedef __attribute__((__vector_size__(4 * sizeof(unsigned)))) unsigned u32x4;   // (an array of uint4 went to scratch memory)
 
 static constexpr int DH = 128;
 static constexpr int BKV = 64;            // keys per tile of the tile kernel
@@ -84,26 +85,24 @@ struct Score {
   }
 };
 
-// 16 bytes of a value row: halves that are not finite become zeros (they would turn a weight of 0 into NaN); true if there was one.
-__device__ inline bool only_finite(uint4& v) {
-  bool bad = false;
-  uint32_t* const w = reinterpret_cast<uint32_t*>(&v);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if ((w[i] & 0x7f80u) == 0x7f80u) { w[i] &= 0xffff0000u; bad = true; }
-    if ((w[i] & 0x7f800000u) == 0x7f800000u) { w[i] &= 0xffffu; bad = true; }
-  }
-  return bad;
+// Two values: halves that are not finite become zeros (they would turn a weight of 0 into NaN); bad: there was one.
+__device__ inline uint32_t only_finite(uint32_t w, bool& bad) {
+  const bool lo = (w & 0x7f80u) == 0x7f80u, hi = (w & 0x7f800000u) == 0x7f800000u;
+  bad |= lo | hi;
+  return w & (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
 }
-// What such values of keys key0 .. key0 + n - 1 add to the columns that see them: an infinity or NaN, whatever the weight.
-__device__ __forceinline__ void add_not_finite(const bf16* v_pool, KvGeom g, int seq, int kvh, int key0, int n, Range r, f32x16 (&acc_o)[4]) {
+__device__ inline u32x4 only_finite(u32x4 v, bool& bad) {
+  return u32x4{only_finite(v[0], bad), only_finite(v[1], bad), only_finite(v[2], bad), only_finite(v[3], bad)};
+}
+// What such values of keys key0 .. key1 - 1 add to the columns that see them: an infinity or NaN, whatever the weight.  Behind the main loop, over
+// the whole range, in the rare case that the staging met one.
+__device__ __forceinline__ void add_not_finite(const bf16* v_pool, const KvGeom& g, int seq, int kvh, int key0, int key1, Range r, f32x16 (&acc_o)[4]) {
   const int half = (threadIdx.x >> 5) & 1;
 #pragma unroll 1
-  for (int j = 0; j < n; ++j) {
-    const int key = key0 + j;
-    if (!__any(r.lo <= key && key <= r.hi)) continue;
-    const bf16* const v = v_pool + kv_row_offset(g, seq, key, kvh) + 4 * half;
+  for (int key = key0; key < key1; ++key) {
     const bool sees = r.lo <= key && key <= r.hi;
+    if (!__any(sees)) continue;
+    const bf16* const v = v_pool + kv_row_offset(g, seq, key, kvh) + 4 * half;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -180,7 +179,7 @@ template <bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2)
 masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][BKV * 256];   // [buffer][K, V]
-  __shared__ int bad_v[2][4];
+  __shared__ int bad_v;
   const int kvh = (int)blockIdx.x % a.g.n_kv_heads;
   const int item = (int)blockIdx.x / a.g.n_kv_heads;
   const int slot = n_slots - 1 - item / sp.n_chunks, chunk = item % sp.n_chunks;   // late rows see the most keys: they go first
@@ -232,14 +231,14 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     const int key = min(t * BKV + lane, a.max_len - 1), at = block_of(a.g, key);
     return {table[min(at, a.g.max_blocks - 1)], key - at * a.g.block_size};
   };
-  uint4 rk[4], rv[4];
+  u32x4 rk[4], rv[4];
   auto fetch = [&](Asked q) __attribute__((always_inline)) {
     const unsigned pool_row = (unsigned)(min(max(q.block, 0), a.g.n_blocks - 1) * a.g.n_kv_heads + kvh) * (unsigned)a.g.block_size + q.slot;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const size_t off = (size_t)(unsigned)__shfl((int)pool_row, (tid >> 4) + 16 * i, 64) * 256 + (tid & 15) * 16;
-      rk[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.k_pool) + off);
-      rv[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.v_pool) + off);
+      rk[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.k_pool) + off);
+      rv[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.v_pool) + off);
     }
   };
   auto whole = [&](int t) { return t * BKV >= lo_max && t * BKV + BKV - 1 <= hi_min; };   // every row of the tile sees all of its keys
@@ -247,16 +246,15 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     bool bad = false;
     if (!whole(t)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bad |= only_finite(rv[i]);
+      for (int i = 0; i < 4; ++i) rv[i] = only_finite(rv[i], bad);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int key = (tid >> 4) + 16 * i, piece = tid & 15;
-      *reinterpret_cast<uint4*>(&lds[buf][0][key * 256 + 16 * (piece ^ (key & 15))]) = rk[i];
-      *reinterpret_cast<uint4*>(&lds[buf][1][key * 256 + 16 * (piece ^ (4 * (key & 3)))]) = rv[i];
+      *reinterpret_cast<u32x4*>(&lds[buf][0][key * 256 + 16 * (piece ^ (key & 15))]) = rk[i];
+      *reinterpret_cast<u32x4*>(&lds[buf][1][key * 256 + 16 * (piece ^ (4 * (key & 3)))]) = rv[i];
     }
-    const bool any_bad = __any(bad);
-    if (lane == 0) bad_v[buf][wave] = any_bad;
+    if (bad) bad_v = 1;
   };
 
   f32x16 acc_o[4];
@@ -266,6 +264,8 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
 
+  if (tid == 0) bad_v = 0;
+  __syncthreads();
   if (t_begin < t_end) {
     fetch(ask(t_begin));
     const Asked second = ask(t_begin + 1);
@@ -310,9 +310,11 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
 #pragma unroll
       for (int db = 0; db < 4; ++db)
         acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(v, lane, u, db), p[u], acc_o[db], 0, 0, 0);
-    if (!whole(t) && (bad_v[buf][0] | bad_v[buf][1] | bad_v[buf][2] | bad_v[buf][3]))
-      add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, t * BKV, min(BKV, a.max_len - t * BKV), mine, acc_o);
     __syncthreads();   // tile t consumed, tile t + 1 staged
+  }
+  if (bad_v) {
+    // whole tiles were not looked at and have multiplied theirs: once more does no harm
+    add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, t_begin * BKV, min(t_end * BKV, a.max_len), mine, acc_o);
   }
 
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
@@ -386,16 +388,16 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
     const int key = min(min(b, b_end - 1) * ROW_KEYS + col, a.max_len - 1), at = block_of(a.g, key);
     return {table[min(at, a.g.max_blocks - 1)], key - at * a.g.block_size};
   };
-  uint4 rk[8], rv[8];
+  u32x4 rk[8], rv[8];
   auto fetch = [&](Asked q) __attribute__((always_inline)) {
     const unsigned pool_row = (unsigned)(min(max(q.block, 0), a.g.n_blocks - 1) * a.g.n_kv_heads + kvh) * (unsigned)a.g.block_size + q.slot;
     size_t off[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) off[i] = (size_t)(unsigned)__shfl((int)pool_row, 4 * i + (lane >> 4), 64) * 256 + (lane & 15) * 16;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rk[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.k_pool) + off[i]);
+    for (int i = 0; i < 8; ++i) rk[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.k_pool) + off[i]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) rv[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(a.v_pool) + off[i]);
+    for (int i = 0; i < 8; ++i) rv[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.v_pool) + off[i]);
   };
 
   f32x16 acc_o[4];
@@ -407,23 +409,23 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
   unsigned char* const k = lds_rows + wave * kRowWaveBytes;
   unsigned char* const v = k + ROW_KEYS * 256;
   int b = b_begin + wave;
+  bool bad = false;
   if (b < b_end) {
     Asked next = ask(b);
     fetch(next);
     next = ask(b + 4);
     for (; b < b_end; b += 4) {
       const bool whole = b * ROW_KEYS >= lo_max && b * ROW_KEYS + ROW_KEYS - 1 <= hi_min;
-      bool bad = false;
       if (!whole) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bad |= only_finite(rv[i]);
+        for (int i = 0; i < 8; ++i) rv[i] = only_finite(rv[i], bad);
       }
       // this wavefront's own memory, and its LDS accesses stay in order: no barrier
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = 4 * i + (lane >> 4), piece = lane & 15;
-        *reinterpret_cast<uint4*>(k + key * 256 + 16 * (piece ^ (key & 15))) = rk[i];
-        *reinterpret_cast<uint4*>(v + key * 256 + 16 * (piece ^ (4 * (key & 3)))) = rv[i];
+        *reinterpret_cast<u32x4*>(k + key * 256 + 16 * (piece ^ (key & 15))) = rk[i];
+        *reinterpret_cast<u32x4*>(v + key * 256 + 16 * (piece ^ (4 * (key & 3)))) = rv[i];
       }
       asm volatile("" ::: "memory");
       if (b + 4 < b_end) {
@@ -452,9 +454,11 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
 #pragma unroll
         for (int db = 0; db < 4; ++db)
           acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(v, lane, u, db), p[u], acc_o[db], 0, 0, 0);
-      if (__any(bad))
-        add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, b * ROW_KEYS, min(ROW_KEYS, a.max_len - b * ROW_KEYS), mine, acc_o);
       asm volatile("" ::: "memory");
+    }
+    if (__any(bad)) {
+      for (b = b_begin + wave; b < b_end; b += 4)
+        add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, b * ROW_KEYS, min(b * ROW_KEYS + ROW_KEYS, a.max_len), mine, acc_o);
     }
   }
 
