@@ -7,8 +7,8 @@
 // permutation of the keys inside a group of 16 (a lane of half h has keys 4h .. 4h + 3 and 8 + 4h .. 8 + 4h + 3); the transposing read
 // takes four keys at a time, so it follows that order for nothing.
 //
-// In LDS a row is 256 bytes; its 16-byte pieces change places by the key: K's piece c is at c ^ (key & 15), which lets eight (sixteen) lanes that
-// fetch one piece of consecutive keys meet every bank once, V's at c ^ 4 (key & 3), which does so for the four keys of a transposing read.
+// Rows in LDS are padded: K's lie 272 bytes apart, so that the lanes that fetch one 16-byte piece of consecutive keys meet every bank once, V's 320, which
+// does so for the four keys of a transposing read; every address is a lane's base plus a constant (SQ_LDS_BANK_CONFLICT: 0).
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -28,7 +28,10 @@ static constexpr int BKV = 64;            // keys per tile of the tile kernel
 static constexpr int TILE_COLS = 128;     // columns of a tile: four wavefronts, 32 each
 static constexpr int ROW_COLS = 32;       // columns of the few-row kernel
 static constexpr int ROW_KEYS = 32;       // keys a wavefront of it takes at a time
+static constexpr int KROW = DH * 2 + 16, VROW = DH * 2 + 64;   // bytes between rows in LDS
 static constexpr int PROW = DH + 4;       // floats between the columns of a partial result
+static constexpr int K_TILE = BKV * KROW, V_TILE = BKV * VROW, kTileBytes = 2 * (K_TILE + V_TILE);
+static constexpr int kAhead = 4;          // LDS operand fragments in flight ahead of the product that uses them
 static constexpr float kRescaleSlack = 8.f;   // log2 units the running maximum may lead the reference exponent
 static constexpr float kLog2e = 1.4426950408889634f;
 
@@ -69,20 +72,25 @@ __device__ inline int last_at_or_before(int n, int x, F start) {
   }
 }
 
-// Scores in units of log2: what a weight is 2 to the power of.
+// Scores in units of log2 (what a weight is 2 to the power of), up to a line: score = raw * MUL + add, MUL and add the same for all keys, so
+// that the line and the reference exponent's subtraction are one operation.  The cap: cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1), whose
+// quotient is the raw score (it falls as the score rises); its error of 2^-23 changes a weight by as much times the cap, where weights are
+// rounded to 2^-9 in any case.
 template <bool CAP, bool BIAS>
 struct Score {
-  float scale, twice, cap, slope, from;   // from: key offset of the lane's element 0 minus the row's position
-  // the cap's tanh(x / cap) = 1 - 2 / (exp(2 x / cap) + 1): an error of 2^-23 of the cap, a weight's relative error of as much times the cap, where
-  // the weight is rounded to 2^-8 in any case
-  __device__ Score(const MaskedAttnArgs& a) : scale(a.scale * kLog2e), twice(CAP ? 2.f * kLog2e * a.scale / a.cap : 0.f), cap(a.cap * kLog2e), slope(0.f), from(0.f) {}
-  __device__ float operator()(float dot, float offset) const {
-    float x;
-    if constexpr (CAP) x = fmaf(-2.f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(dot * twice) + 1.f), cap);
-    else x = dot * scale;
-    if constexpr (BIAS) x = fmaf(-slope, fabsf(from + offset), x);
+  static constexpr bool kFalls = CAP && !BIAS;
+  float in, out, mul, add, slope, from;   // from: key offset of the lane's element 0 minus the row's position
+  __device__ Score(const MaskedAttnArgs& a)
+      : in(CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e), out(-2.f * kLog2e * a.cap),
+        mul(BIAS ? 1.f : CAP ? out : in), add(CAP ? kLog2e * a.cap : 0.f), slope(0.f), from(0.f) {}
+  __device__ __forceinline__ float raw(float dot, float offset) const {
+    float x = dot;
+    if constexpr (CAP) x = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(x * in) + 1.f);
+    if constexpr (BIAS) x = fmaf(-slope, fabsf(from + offset), x * (CAP ? out : in));
     return x;
   }
+  static __device__ __forceinline__ float none() { return kFalls ? INFINITY : -INFINITY; }   // the raw score of a key that is not seen
+  static __device__ __forceinline__ float larger(float x, float y) { return kFalls ? fminf(x, y) : fmaxf(x, y); }
 };
 
 // Two values: halves that are not finite become zeros (they would turn a weight of 0 into NaN); bad: there was one.
@@ -113,17 +121,17 @@ __device__ __forceinline__ void add_not_finite(const bf16* v_pool, const KvGeom&
   }
 }
 
-// The running softmax of a column over 16 B keys (B blocks of 32 scores, in two lanes): scores become weights.
-// The reference exponent follows the maximum lazily: the sums are rescaled only when a column's maximum has grown by more than
-// kRescaleSlack since the last time, so weights stay below 2^kRescaleSlack instead of 1; any reference gives the same quotient.
-template <int B>
-__device__ __forceinline__ void online_softmax(f32x16 (&s)[B], float& m_run, float& l_run, f32x16 (&acc_o)[4], bf16x8 (&p)[2 * B]) {
+// The running softmax of a column over 32 B keys (in two lanes).  The reference exponent follows the maximum lazily: the sums are rescaled only
+// when a column's maximum has grown by more than kRescaleSlack since the last time, so weights stay below 2^kRescaleSlack instead of 1; any
+// reference gives the same quotient.
+template <bool CAP, bool BIAS, int B>
+__device__ __forceinline__ float move_reference(const Score<CAP, BIAS>& score, const f32x16 (&s)[B], float& m_run, float& l_run, f32x16 (&acc_o)[4]) {
   float mx = s[0][0];
 #pragma unroll
   for (int b = 0; b < B; ++b)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[b][e]);
-  mx = pair_max(mx);
+    for (int e = 0; e < 16; ++e) mx = Score<CAP, BIAS>::larger(mx, s[b][e]);
+  mx = pair_max(fmaf(mx, score.mul, score.add));
   const float m_new = fmaxf(m_run, mx);
   if (__any(m_new > m_run + kRescaleSlack)) {
     const float corr = __builtin_amdgcn_exp2f(m_run - (m_new == -INFINITY ? 0.f : m_new));
@@ -134,35 +142,33 @@ __device__ __forceinline__ void online_softmax(f32x16 (&s)[B], float& m_run, flo
       for (int e = 0; e < 16; ++e) acc_o[i][e] *= corr;
     m_run = m_new;
   }
-  const float m_use = m_run == -INFINITY ? 0.f : m_run;
-  float sum = 0.f;
+  return score.add - (m_run == -INFINITY ? 0.f : m_run);
+}
+// the weights of eight scores, rounded for the product; the sum takes them as they are
+template <bool CAP, bool BIAS>
+__device__ __forceinline__ bf16x8 weights(const Score<CAP, BIAS>& score, const f32x16& s, int u, float add, float& sum) {
+  f32x8 w;
 #pragma unroll
-  for (int u = 0; u < 2 * B; ++u) {
-    f32x8 w;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = __builtin_amdgcn_exp2f(s[u >> 1][8 * (u & 1) + j] - m_use);
-      sum += w[j];
-    }
-    p[u] = __builtin_convertvector(w, bf16x8);   // rounded for the product; the sum takes them as they are
+  for (int j = 0; j < 8; ++j) {
+    w[j] = __builtin_amdgcn_exp2f(fmaf(s[8 * u + j], score.mul, add));
+    sum += w[j];
   }
-  l_run += sum;
+  return __builtin_convertvector(w, bf16x8);
 }
 
-__device__ inline bf16x8 k_fragment(const unsigned char* k, int key, int piece) {
-  return __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k + key * 256 + 16 * (piece ^ (key & 15))));
+// K operand: key block b (32 keys), d step i (16 of them); k: the lane's place, kv_lane_k
+__device__ __forceinline__ int k_lane(int lane) { return (lane & 31) * KROW + (lane >> 5) * 16; }
+__device__ __forceinline__ bf16x8 k_fragment(const unsigned char* k, int b, int i) {
+  return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(k + b * 32 * KROW + 32 * i));
 }
-// V^T operand of keys 16 t .. 16 t + 15 and d = 32 db .. 32 db + 31
-__device__ inline bf16x8 v_fragment(const unsigned char* v, int lane, int t, int db) {
-  const int key = 16 * t + 4 * (lane >> 5) + ((lane >> 2) & 3);
-  const int byte = 64 * db + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-  auto at = [&](int k) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4*)(v + k * 256 + (byte ^ (64 * (k & 3)))));
-  };
-  const s16x4 a = at(key), b = at(key + 8);
+// V^T operand of keys 16 t .. 16 t + 15 and d = 32 db .. 32 db + 31; v: the lane's place
+__device__ __forceinline__ int v_lane(int lane) { return (4 * (lane >> 5) + ((lane >> 2) & 3)) * VROW + 32 * ((lane >> 4) & 1) + 8 * (lane & 3); }
+__device__ __forceinline__ bf16x8 v_fragment(const unsigned char* v, int t, int db) {
   typedef __attribute__((__vector_size__(8 * sizeof(short)))) short s16x8;
-  return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  auto at = [&](int key) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(v + key * VROW + 64 * db));
+  };
+  return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(at(16 * t), at(16 * t + 8), 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // how a batch's key ranges are cut
@@ -178,7 +184,7 @@ __device__ inline uint2 pack4(float a, float b, float c, float d) {
 template <bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2)
 masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, float* __restrict__ part_o, float2* __restrict__ part_ml) {
-  __shared__ __attribute__((aligned(16))) unsigned char lds[2][2][BKV * 256];   // [buffer][K, V]
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];   // two K tiles, two V tiles
   __shared__ int bad_v;
   const int kvh = (int)blockIdx.x % a.g.n_kv_heads;
   const int item = (int)blockIdx.x / a.g.n_kv_heads;
@@ -224,36 +230,56 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
   const int pos = a.row_pos[row];
 
-  // A lane looks up the pool row of one key of a tile, two tiles ahead; a thread loads 16 bytes of four rows.
+  // A lane looks up the block of one key of a tile, three tiles ahead; a thread loads 16 bytes of four rows.  In blocks of 16, 32, 64, ... slots (or one
+  // block a sequence) the 16 keys of a group lie one behind the other, and loads go to a group's scalar address and a constant lane offset.
   const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
+  const bool by_group = a.g.max_blocks == 1 || a.g.bs_shift >= 4;
+  const int max_key = a.max_len - 1, last_block = a.g.max_blocks - 1, block_size = a.g.block_size, head_rows = a.g.n_kv_heads, pool_blocks = a.g.n_blocks - 1;
+  const KvGeom geom = a.g;
+  const char* const k_pool = reinterpret_cast<const char*>(a.k_pool);
+  const char* const v_pool = reinterpret_cast<const char*>(a.v_pool);
   struct Asked { int block, slot; };
   auto ask = [&](int t) __attribute__((always_inline)) -> Asked {
-    const int key = min(t * BKV + lane, a.max_len - 1), at = block_of(a.g, key);
-    return {table[min(at, a.g.max_blocks - 1)], key - at * a.g.block_size};
+    const int key = min(t * BKV + lane, max_key), at = block_of(geom, key);
+    return {table[min(at, last_block)], key - at * block_size};
   };
+  auto row_of = [&](Asked q) __attribute__((always_inline)) { return (unsigned)(min(max(q.block, 0), pool_blocks) * head_rows + kvh) * (unsigned)block_size + q.slot; };
   u32x4 rk[4], rv[4];
-  auto fetch = [&](Asked q) __attribute__((always_inline)) {
-    const unsigned pool_row = (unsigned)(min(max(q.block, 0), a.g.n_blocks - 1) * a.g.n_kv_heads + kvh) * (unsigned)a.g.block_size + q.slot;
+  const unsigned lane_off = (tid >> 4) * 256 + (tid & 15) * 16;
+  auto group_row = [&](unsigned row, int i) __attribute__((always_inline)) { return (size_t)(unsigned)__builtin_amdgcn_readlane((int)row, 16 * i) * 256; };
+  auto load = [&](const char* pool, size_t row) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(pool + row + lane_off); };
+  // the last tile of a range may end inside a group whose rest lies past max_key: its rows are handed around
+  auto grouped = [&](int t) __attribute__((always_inline)) { return by_group && t * BKV + BKV - 1 <= max_key; };
+  auto fetch = [&](int t, Asked q) __attribute__((always_inline)) {
+    const unsigned row = row_of(q);
+    if (grouped(t)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const size_t off = (size_t)(unsigned)__shfl((int)pool_row, (tid >> 4) + 16 * i, 64) * 256 + (tid & 15) * 16;
-      rk[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.k_pool) + off);
-      rv[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.v_pool) + off);
+      for (int i = 0; i < 4; ++i) { rk[i] = load(k_pool, group_row(row, i)); rv[i] = load(v_pool, group_row(row, i)); }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const size_t off = (size_t)(unsigned)__shfl((int)row, (tid >> 4) + 16 * i, 64) * 256 + (tid & 15) * 16;
+        rk[i] = *reinterpret_cast<const u32x4*>(k_pool + off);
+        rv[i] = *reinterpret_cast<const u32x4*>(v_pool + off);
+      }
     }
   };
-  auto whole = [&](int t) { return t * BKV >= lo_max && t * BKV + BKV - 1 <= hi_min; };   // every row of the tile sees all of its keys
-  auto stage = [&](int t, int buf) __attribute__((always_inline)) {
+  // tiles t_whole .. t_ragged - 1: every row of the tile sees all of their keys
+  const int t_whole = (lo_max + BKV - 1) / BKV, t_ragged = (hi_min + 1) / BKV;
+  unsigned char* const k_wr = lds + (tid >> 4) * KROW + (tid & 15) * 16;
+  unsigned char* const v_wr = lds + 2 * K_TILE + (tid >> 4) * VROW + (tid & 15) * 16;
+  auto stage_k = [&](auto buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(k_wr + decltype(buf)::value * K_TILE + i * 16 * KROW) = rk[i];
+  };
+  auto stage_v = [&](auto buf, int i) __attribute__((always_inline)) {
+    *reinterpret_cast<u32x4*>(v_wr + decltype(buf)::value * V_TILE + i * 16 * VROW) = rv[i];
+  };
+  auto clean_v = [&](int t) __attribute__((always_inline)) {
+    if (t >= t_whole && t < t_ragged) return;
     bool bad = false;
-    if (!whole(t)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) rv[i] = only_finite(rv[i], bad);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = (tid >> 4) + 16 * i, piece = tid & 15;
-      *reinterpret_cast<u32x4*>(&lds[buf][0][key * 256 + 16 * (piece ^ (key & 15))]) = rk[i];
-      *reinterpret_cast<u32x4*>(&lds[buf][1][key * 256 + 16 * (piece ^ (4 * (key & 3)))]) = rv[i];
-    }
+    for (int i = 0; i < 4; ++i) rv[i] = only_finite(rv[i], bad);
     if (bad) bad_v = 1;
   };
 
@@ -264,53 +290,118 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
 
+  const std::integral_constant<int, 0> buf0;
+  const std::integral_constant<int, 1> buf1;
+  Asked asked = {};   // of the tile two on
   if (tid == 0) bad_v = 0;
-  __syncthreads();
   if (t_begin < t_end) {
-    fetch(ask(t_begin));
-    const Asked second = ask(t_begin + 1);
-    stage(t_begin, 0);
-    fetch(second);
+    const Asked q0 = ask(t_begin), q1 = ask(t_begin + 1);
+    asked = ask(t_begin + 2);
+    fetch(t_begin, q0);
+    __syncthreads();
+    clean_v(t_begin);
+    stage_k(buf0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) stage_v(buf0, i);
+    fetch(t_begin + 1, q1);
   }
   __syncthreads();
-  for (int t = t_begin; t < t_end; ++t) {
-    const int buf = (t - t_begin) & 1;
-    const unsigned char* const k = lds[buf][0];
-    const unsigned char* const v = lds[buf][1];
-    const Asked next2 = ask(t + 2);
+  const unsigned char* const k_rd = lds + k_lane(lane);
+  const unsigned char* const v_rd = lds + 2 * K_TILE + v_lane(lane);
+  // Step t multiplies the tile in buffer t % 2 (counted from t_begin), stages tile t + 1, whose rows are in registers, into the other and asks for tile t + 2.
+  // steady: t and t + 1 are whole tiles, t + 2 grouped and there.
+  auto tile_step = [&](int t, auto buf, auto steady_) __attribute__((always_inline)) {
+    constexpr bool steady = decltype(steady_)::value;
+    constexpr int KOFF = decltype(buf)::value * K_TILE, VOFF = decltype(buf)::value * V_TILE;
+    const std::integral_constant<int, 1 - decltype(buf)::value> other;
+    const unsigned row2 = row_of(asked);
+    const Asked asked2 = asked;
+    asked = ask(t + 3);
     f32x16 acc_s[2];
+    {
+      f32x16 zero;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+      bf16x8 kf[kAhead];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc_s[b][e] = 0.f;
+      for (int i = 0; i < kAhead; ++i) kf[i] = k_fragment(k_rd + KOFF, i & 1, i >> 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 16; ++i) {
+        acc_s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % kAhead], qf[i >> 1], i < 2 ? zero : acc_s[i & 1], 0, 0, 0);
+        if (i + kAhead < 16) kf[i % kAhead] = k_fragment(k_rd + KOFF, (i + kAhead) & 1, (i + kAhead) >> 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    bf16x8 vf[kAhead];
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-        acc_s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(k, 32 * b + ql, 2 * i + half), qf[i], acc_s[b], 0, 0, 0);
-    if (t + 1 < t_end) stage(t + 1, buf ^ 1);
-    if (t + 2 < t_end) fetch(next2);
+    for (int i = 0; i < kAhead; ++i) vf[i] = v_fragment(v_rd + VOFF, i >> 2, i & 3);
+    __builtin_amdgcn_sched_barrier(0);
+    if (steady) {
+      stage_k(other);
+    } else if (t + 1 < t_end) {
+      clean_v(t + 1);
+      stage_k(other);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) stage_v(other, i);
+    }
+    if (!steady && t + 2 < t_end) fetch(t + 2, asked2);
     if constexpr (BIAS) score.from = (float)(t * BKV + 4 * half - pos);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc_s[b][e] = score(acc_s[b][e], (float)(32 * b + 8 * (e >> 2) + (e & 3)));
-    if (!whole(t)) {
+      for (int e = 0; e < 16; ++e) acc_s[b][e] = score.raw(acc_s[b][e], (float)(32 * b + 8 * (e >> 2) + (e & 3)));
+    if (!steady && (t < t_whole || t >= t_ragged)) {
       const int key0 = t * BKV + 4 * half - mine.lo;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if ((unsigned)(key0 + 32 * b + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[b][e] = -INFINITY;
+          if ((unsigned)(key0 + 32 * b + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[b][e] = score.none();
     }
+    const float add = move_reference(score, acc_s, m_run, l_run, acc_o);
     bf16x8 p[4];
-    online_softmax<2>(acc_s, m_run, l_run, acc_o, p);
+    float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < 4; ++u) {
+      p[u] = weights(score, acc_s[u >> 1], u & 1, add, sum);
+      asm volatile("" : "+v"(sum));   // added up here, or the 32 weights stay in registers over the second product
+      if constexpr (steady) {
+        __builtin_amdgcn_sched_barrier(0);
+        stage_v(other, u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    l_run += sum;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int db = 0; db < 4; ++db)
-        acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(v, lane, u, db), p[u], acc_o[db], 0, 0, 0);
+    for (int i = 0; i < 16; ++i) {
+      acc_o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kAhead], p[i >> 2], acc_o[i & 3], 0, 0, 0);
+      if (i + kAhead < 16) vf[i % kAhead] = v_fragment(v_rd + VOFF, (i + kAhead) >> 2, (i + kAhead) & 3);
+      if constexpr (steady) {
+        if (i % 4 == 0) rk[i / 4] = load(k_pool, group_row(row2, i / 4));
+        if (i % 4 == 2) rv[i / 4] = load(v_pool, group_row(row2, i / 4));
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     __syncthreads();   // tile t consumed, tile t + 1 staged
+  };
+  int t = t_begin;
+  const std::true_type steady;
+  const std::false_type general;
+  // steady tiles come in pairs, from an even number of steps on
+  const int t_steady = by_group ? min(min(t_ragged - 1, t_end - 2), (max_key + 1) / BKV - 2) : 0;   // tiles before it may run steadily
+  while (t < t_end) {
+    if (t >= t_whole && t + 1 < t_steady) {
+      for (; t + 1 < t_steady; t += 2) {
+        tile_step(t, buf0, steady);
+        tile_step(t + 1, buf1, steady);
+      }
+    } else {
+      tile_step(t, buf0, general);
+      if (t + 1 < t_end) tile_step(t + 1, buf1, general);
+      t += 2;
+    }
   }
   if (bad_v) {
     // whole tiles were not looked at and have multiplied theirs: once more does no harm
@@ -342,7 +433,8 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
 // ------------------------------------------------------------------ few rows a sequence: at most 32 columns
 // A workgroup takes a sequence's columns and a range of keys; its wavefronts take every fourth block of 32 keys of the range with a softmax of
 // their own and share nothing before the end.
-static constexpr int kRowWaveBytes = ROW_COLS * PROW * 4;   // a wavefront's K and V (16 KB), at the end its sums
+static constexpr int kRowWaveBytes = ROW_KEYS * (KROW + VROW);   // a wavefront's K and V, at the end its sums
+static_assert(kRowWaveBytes >= ROW_COLS * PROW * 4, "room for the sums");
 template <bool CAP, bool BIAS>
 __global__ void __launch_bounds__(256, 2)
 masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ part_o, float2* __restrict__ part_ml) {
@@ -407,7 +499,7 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
     for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
   unsigned char* const k = lds_rows + wave * kRowWaveBytes;
-  unsigned char* const v = k + ROW_KEYS * 256;
+  unsigned char* const v = k + ROW_KEYS * KROW;
   int b = b_begin + wave;
   bool bad = false;
   if (b < b_end) {
@@ -424,8 +516,8 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = 4 * i + (lane >> 4), piece = lane & 15;
-        *reinterpret_cast<u32x4*>(k + key * 256 + 16 * (piece ^ (key & 15))) = rk[i];
-        *reinterpret_cast<u32x4*>(v + key * 256 + 16 * (piece ^ (4 * (key & 3)))) = rv[i];
+        *reinterpret_cast<u32x4*>(k + key * KROW + 16 * piece) = rk[i];
+        *reinterpret_cast<u32x4*>(v + key * VROW + 16 * piece) = rv[i];
       }
       asm volatile("" ::: "memory");
       if (b + 4 < b_end) {
@@ -437,23 +529,25 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
       for (int e = 0; e < 16; ++e) acc_s[0][e] = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        acc_s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(k, col, 2 * i + half), qf[i], acc_s[0], 0, 0, 0);
+        acc_s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_fragment(k + k_lane(lane), 0, i), qf[i], acc_s[0], 0, 0, 0);
       if constexpr (BIAS) score.from = (float)(b * ROW_KEYS + 4 * half - pos);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc_s[0][e] = score(acc_s[0][e], (float)(8 * (e >> 2) + (e & 3)));
+      for (int e = 0; e < 16; ++e) acc_s[0][e] = score.raw(acc_s[0][e], (float)(8 * (e >> 2) + (e & 3)));
       if (!whole) {
         const int key0 = b * ROW_KEYS + 4 * half - mine.lo;
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if ((unsigned)(key0 + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[0][e] = -INFINITY;
+          if ((unsigned)(key0 + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[0][e] = score.none();
       }
       bf16x8 p[2];
-      online_softmax<1>(acc_s, m_run, l_run, acc_o, p);
+      const float add = move_reference(score, acc_s, m_run, l_run, acc_o);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) p[u] = weights(score, acc_s[0], u, add, l_run);
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int db = 0; db < 4; ++db)
-          acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(v, lane, u, db), p[u], acc_o[db], 0, 0, 0);
+          acc_o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_fragment(v + v_lane(lane), u, db), p[u], acc_o[db], 0, 0, 0);
       asm volatile("" ::: "memory");
     }
     if (__any(bad)) {
@@ -635,7 +729,10 @@ static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, floa
     if (e != hipSuccess) return e;
     masked_attn_rows_kernel<CAP, BIAS><<<(unsigned)grid, 256, 4 * kRowWaveBytes, st>>>(a, p.split, part_o, part_ml);
   } else {
-    masked_attn_tile_kernel<CAP, BIAS><<<(unsigned)grid, 256, 0, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
+    static std::atomic<unsigned long long> told{0};
+    const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<CAP, BIAS>, kTileBytes, told);
+    if (e != hipSuccess) return e;
+    masked_attn_tile_kernel<CAP, BIAS><<<(unsigned)grid, 256, kTileBytes, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
   }
   return hipGetLastError();
 }
