@@ -181,7 +181,7 @@ __device__ inline uint2 pack4(float a, float b, float c, float d) {
 // ------------------------------------------------------------------ tiles of 128 columns
 // Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
 // over the sequences (ceil(n / R) <= floor((a + n) / R) - floor(a / R) + 1).
-template <bool CAP, bool BIAS>
+template <bool CAP, bool BIAS, bool GROUPED>
 __global__ void __launch_bounds__(256, 2)
 masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];   // two K tiles, two V tiles
@@ -230,38 +230,35 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
   const int pos = a.row_pos[row];
 
-  // A lane looks up the block of one key of a tile, three tiles ahead; a thread loads 16 bytes of four rows.  In blocks of 16, 32, 64, ... slots (or one
-  // block a sequence) the 16 keys of a group lie one behind the other, and loads go to a group's scalar address and a constant lane offset.
+  // A lane looks up the block of one key of a tile, three tiles ahead; a thread loads 16 bytes of four rows.  GROUPED: the 16 keys of a group lie one
+  // behind the other, so that loads go to a group's scalar address and a constant lane offset; else every key's row is handed around.  Behind
+  // the last key that one is repeated (its group).
   const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
-  const bool by_group = a.g.max_blocks == 1 || a.g.bs_shift >= 4;
-  const int max_key = a.max_len - 1, last_block = a.g.max_blocks - 1, block_size = a.g.block_size, head_rows = a.g.n_kv_heads, pool_blocks = a.g.n_blocks - 1;
+  const int last_key = min(t_end * BKV, a.max_len) - 1, ask_key = GROUPED ? last_key & ~15 : last_key;
+  const int last_block = a.g.max_blocks - 1, block_size = a.g.block_size, head_rows = a.g.n_kv_heads, pool_blocks = a.g.n_blocks - 1;
   const KvGeom geom = a.g;
   const char* const k_pool = reinterpret_cast<const char*>(a.k_pool);
   const char* const v_pool = reinterpret_cast<const char*>(a.v_pool);
   struct Asked { int block, slot; };
   auto ask = [&](int t) __attribute__((always_inline)) -> Asked {
-    const int key = min(t * BKV + lane, max_key), at = block_of(geom, key);
+    const int key = min(t * BKV + lane, ask_key), at = block_of(geom, key);
     return {table[min(at, last_block)], key - at * block_size};
   };
   auto row_of = [&](Asked q) __attribute__((always_inline)) { return (unsigned)(min(max(q.block, 0), pool_blocks) * head_rows + kvh) * (unsigned)block_size + q.slot; };
   u32x4 rk[4], rv[4];
-  const unsigned lane_off = (tid >> 4) * 256 + (tid & 15) * 16;
-  auto group_row = [&](unsigned row, int i) __attribute__((always_inline)) { return (size_t)(unsigned)__builtin_amdgcn_readlane((int)row, 16 * i) * 256; };
-  auto load = [&](const char* pool, size_t row) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(pool + row + lane_off); };
-  // the last tile of a range may end inside a group whose rest lies past max_key: its rows are handed around
-  auto grouped = [&](int t) __attribute__((always_inline)) { return by_group && t * BKV + BKV - 1 <= max_key; };
-  auto fetch = [&](int t, Asked q) __attribute__((always_inline)) {
+  const unsigned lane_off = (GROUPED ? (tid >> 4) * 256 : 0) + (tid & 15) * 16;
+  auto row_bytes = [&](unsigned row, int i) __attribute__((always_inline)) -> size_t {
+    if constexpr (GROUPED) return (size_t)(unsigned)__builtin_amdgcn_readlane((int)row, 16 * i) * 256;
+    return (size_t)(unsigned)__shfl((int)row, (tid >> 4) + 16 * i, 64) * 256;
+  };
+  auto load = [&](const char* pool, size_t at) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(pool + at + lane_off); };
+  auto fetch = [&](Asked q) __attribute__((always_inline)) {
     const unsigned row = row_of(q);
-    if (grouped(t)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { rk[i] = load(k_pool, group_row(row, i)); rv[i] = load(v_pool, group_row(row, i)); }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const size_t off = (size_t)(unsigned)__shfl((int)row, (tid >> 4) + 16 * i, 64) * 256 + (tid & 15) * 16;
-        rk[i] = *reinterpret_cast<const u32x4*>(k_pool + off);
-        rv[i] = *reinterpret_cast<const u32x4*>(v_pool + off);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const size_t at = row_bytes(row, i);
+      rk[i] = load(k_pool, at);
+      rv[i] = load(v_pool, at);
     }
   };
   // tiles t_whole .. t_ragged - 1: every row of the tile sees all of their keys
@@ -276,7 +273,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     *reinterpret_cast<u32x4*>(v_wr + decltype(buf)::value * V_TILE + i * 16 * VROW) = rv[i];
   };
   auto clean_v = [&](int t) __attribute__((always_inline)) {
-    if (t >= t_whole && t < t_ragged) return;
+    if ((t >= t_whole && t < t_ragged) || t >= t_end) return;
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) rv[i] = only_finite(rv[i], bad);
@@ -297,25 +294,23 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   if (t_begin < t_end) {
     const Asked q0 = ask(t_begin), q1 = ask(t_begin + 1);
     asked = ask(t_begin + 2);
-    fetch(t_begin, q0);
+    fetch(q0);
     __syncthreads();
     clean_v(t_begin);
     stage_k(buf0);
 #pragma unroll
     for (int i = 0; i < 4; ++i) stage_v(buf0, i);
-    fetch(t_begin + 1, q1);
+    fetch(q1);
   }
   __syncthreads();
   const unsigned char* const k_rd = lds + k_lane(lane);
   const unsigned char* const v_rd = lds + 2 * K_TILE + v_lane(lane);
-  // Step t multiplies the tile in buffer t % 2 (counted from t_begin), stages tile t + 1, whose rows are in registers, into the other and asks for tile t + 2.
-  // steady: t and t + 1 are whole tiles, t + 2 grouped and there.
-  auto tile_step = [&](int t, auto buf, auto steady_) __attribute__((always_inline)) {
-    constexpr bool steady = decltype(steady_)::value;
+  // Step t multiplies the tile in buffer t % 2 (counted from t_begin), stages tile t + 1, whose rows are in registers, into the other and asks for tile
+  // t + 2; past the end of the range its last rows once more, which nobody multiplies.
+  auto tile_step = [&](int t, auto buf) __attribute__((always_inline)) {
     constexpr int KOFF = decltype(buf)::value * K_TILE, VOFF = decltype(buf)::value * V_TILE;
     const std::integral_constant<int, 1 - decltype(buf)::value> other;
     const unsigned row2 = row_of(asked);
-    const Asked asked2 = asked;
     asked = ask(t + 3);
     f32x16 acc_s[2];
     {
@@ -337,21 +332,15 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) vf[i] = v_fragment(v_rd + VOFF, i >> 2, i & 3);
     __builtin_amdgcn_sched_barrier(0);
-    if (steady) {
-      stage_k(other);
-    } else if (t + 1 < t_end) {
-      clean_v(t + 1);
-      stage_k(other);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) stage_v(other, i);
-    }
-    if (!steady && t + 2 < t_end) fetch(t + 2, asked2);
+    clean_v(t + 1);
+    stage_k(other);
+    __builtin_amdgcn_sched_barrier(0);
     if constexpr (BIAS) score.from = (float)(t * BKV + 4 * half - pos);
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc_s[b][e] = score.raw(acc_s[b][e], (float)(32 * b + 8 * (e >> 2) + (e & 3)));
-    if (!steady && (t < t_whole || t >= t_ragged)) {
+    if (t < t_whole || t >= t_ragged) {
       const int key0 = t * BKV + 4 * half - mine.lo;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
@@ -366,42 +355,29 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     for (int u = 0; u < 4; ++u) {
       p[u] = weights(score, acc_s[u >> 1], u & 1, add, sum);
       asm volatile("" : "+v"(sum));   // added up here, or the 32 weights stay in registers over the second product
-      if constexpr (steady) {
-        __builtin_amdgcn_sched_barrier(0);
-        stage_v(other, u);
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      __builtin_amdgcn_sched_barrier(0);
+      stage_v(other, u);
+      __builtin_amdgcn_sched_barrier(0);
     }
     l_run += sum;
     __builtin_amdgcn_sched_barrier(0);
+    size_t at = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       acc_o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kAhead], p[i >> 2], acc_o[i & 3], 0, 0, 0);
       if (i + kAhead < 16) vf[i % kAhead] = v_fragment(v_rd + VOFF, (i + kAhead) >> 2, (i + kAhead) & 3);
-      if constexpr (steady) {
-        if (i % 4 == 0) rk[i / 4] = load(k_pool, group_row(row2, i / 4));
-        if (i % 4 == 2) rv[i / 4] = load(v_pool, group_row(row2, i / 4));
+      if (i % 4 == 0) {
+        at = row_bytes(row2, i / 4);
+        rk[i / 4] = load(k_pool, at);
       }
+      if (i % 4 == 2) rv[i / 4] = load(v_pool, at);
       __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();   // tile t consumed, tile t + 1 staged
   };
-  int t = t_begin;
-  const std::true_type steady;
-  const std::false_type general;
-  // steady tiles come in pairs, from an even number of steps on
-  const int t_steady = by_group ? min(min(t_ragged - 1, t_end - 2), (max_key + 1) / BKV - 2) : 0;   // tiles before it may run steadily
-  while (t < t_end) {
-    if (t >= t_whole && t + 1 < t_steady) {
-      for (; t + 1 < t_steady; t += 2) {
-        tile_step(t, buf0, steady);
-        tile_step(t + 1, buf1, steady);
-      }
-    } else {
-      tile_step(t, buf0, general);
-      if (t + 1 < t_end) tile_step(t + 1, buf1, general);
-      t += 2;
-    }
+  for (int t = t_begin; t < t_end; t += 2) {
+    tile_step(t, buf0);
+    if (t + 1 < t_end) tile_step(t + 1, buf1);
   }
   if (bad_v) {
     // whole tiles were not looked at and have multiplied theirs: once more does no harm
@@ -719,6 +695,15 @@ size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16) {
   return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (PROW + 2);
 }
 
+template <bool CAP, bool BIAS, bool GROUPED>
+static hipError_t launch_tiles(const MaskedAttnArgs& a, const MaskedPlan& p, unsigned grid, float* part_o, float2* part_ml, hipStream_t st) {
+  static std::atomic<unsigned long long> told{0};
+  const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<CAP, BIAS, GROUPED>, kTileBytes, told);
+  if (e != hipSuccess) return e;
+  masked_attn_tile_kernel<CAP, BIAS, GROUPED><<<grid, 256, kTileBytes, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
+  return hipGetLastError();
+}
+
 template <bool CAP, bool BIAS>
 static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, float* part_o, float2* part_ml, hipStream_t st) {
   const long grid = (long)p.slots * p.split.n_chunks * a.g.n_kv_heads;
@@ -729,10 +714,10 @@ static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, floa
     if (e != hipSuccess) return e;
     masked_attn_rows_kernel<CAP, BIAS><<<(unsigned)grid, 256, 4 * kRowWaveBytes, st>>>(a, p.split, part_o, part_ml);
   } else {
-    static std::atomic<unsigned long long> told{0};
-    const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<CAP, BIAS>, kTileBytes, told);
-    if (e != hipSuccess) return e;
-    masked_attn_tile_kernel<CAP, BIAS><<<(unsigned)grid, 256, kTileBytes, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
+    // pages of 16, 32, 64, ... slots, or one block a sequence whose slots are a multiple of 16
+    const bool grouped = a.g.max_blocks == 1 ? a.g.block_size % 16 == 0 : a.g.bs_shift >= 4;
+    return grouped ? launch_tiles<CAP, BIAS, true>(a, p, (unsigned)grid, part_o, part_ml, st)
+                   : launch_tiles<CAP, BIAS, false>(a, p, (unsigned)grid, part_o, part_ml, st);
   }
   return hipGetLastError();
 }
