@@ -76,8 +76,13 @@ __device__ inline int last_at_or_before(int n, int x, F start) {
 // that the line and the reference exponent's subtraction are one operation.  The cap: cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1), whose
 // quotient is the raw score (it falls as the score rises); its error of 2^-23 changes a weight by as much times the cap, where weights are
 // rounded to 2^-9 in any case.
-template <bool CAP, bool BIAS>
+// Bounded scores: a cap without a bias bounds them by itself, so that its softmax needs no running maximum: with the reference exponent fixed at half
+// the cap, weights lie between 2^-120 and 2^40 up to kMostBounded, and no score has to wait for another.
+enum ScoreKind : int { kPlain = 0, kBias = 1, kCap = 2, kCapBias = 3, kBounded = 4 };
+static constexpr float kMostBounded = 80.f;   // log2 units: a cap of 55
+template <int KIND>
 struct Score {
+  static constexpr bool CAP = KIND >= kCap, BIAS = KIND == kBias || KIND == kCapBias, kFixed = KIND == kBounded;
   static constexpr bool kFalls = CAP && !BIAS;
   float in, out, mul, add, slope, from;   // from: key offset of the lane's element 0 minus the row's position
   __device__ Score(const MaskedAttnArgs& a)
@@ -91,6 +96,7 @@ struct Score {
   }
   static __device__ __forceinline__ float none() { return kFalls ? INFINITY : -INFINITY; }   // the raw score of a key that is not seen
   static __device__ __forceinline__ float larger(float x, float y) { return kFalls ? fminf(x, y) : fmaxf(x, y); }
+  __device__ __forceinline__ float first_reference() const { return kFixed ? 0.5f * add : -INFINITY; }
 };
 
 // Two values: halves that are not finite become zeros (they would turn a weight of 0 into NaN); bad: there was one.
@@ -124,13 +130,14 @@ __device__ __forceinline__ void add_not_finite(const bf16* v_pool, const KvGeom&
 // The running softmax of a column over 32 B keys (in two lanes).  The reference exponent follows the maximum lazily: the sums are rescaled only
 // when a column's maximum has grown by more than kRescaleSlack since the last time, so weights stay below 2^kRescaleSlack instead of 1; any
 // reference gives the same quotient.
-template <bool CAP, bool BIAS, int B>
-__device__ __forceinline__ float move_reference(const Score<CAP, BIAS>& score, const f32x16 (&s)[B], float& m_run, float& l_run, f32x16 (&acc_o)[4]) {
+template <int KIND, int B>
+__device__ __forceinline__ float move_reference(const Score<KIND>& score, const f32x16 (&s)[B], float& m_run, float& l_run, f32x16 (&acc_o)[4]) {
+  if constexpr (Score<KIND>::kFixed) return score.add - m_run;
   float mx = s[0][0];
 #pragma unroll
   for (int b = 0; b < B; ++b)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) mx = Score<CAP, BIAS>::larger(mx, s[b][e]);
+    for (int e = 0; e < 16; ++e) mx = Score<KIND>::larger(mx, s[b][e]);
   mx = pair_max(fmaf(mx, score.mul, score.add));
   const float m_new = fmaxf(m_run, mx);
   if (__any(m_new > m_run + kRescaleSlack)) {
@@ -145,8 +152,8 @@ __device__ __forceinline__ float move_reference(const Score<CAP, BIAS>& score, c
   return score.add - (m_run == -INFINITY ? 0.f : m_run);
 }
 // the weights of eight scores, rounded for the product; the sum takes them as they are
-template <bool CAP, bool BIAS>
-__device__ __forceinline__ bf16x8 weights(const Score<CAP, BIAS>& score, const f32x16& s, int u, float add, float& sum) {
+template <int KIND>
+__device__ __forceinline__ bf16x8 weights(const Score<KIND>& score, const f32x16& s, int u, float add, float& sum) {
   f32x8 w;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -181,7 +188,7 @@ __device__ inline uint2 pack4(float a, float b, float c, float d) {
 // ------------------------------------------------------------------ tiles of 128 columns
 // Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
 // over the sequences (ceil(n / R) <= floor((a + n) / R) - floor(a / R) + 1).
-template <bool CAP, bool BIAS, bool GROUPED>
+template <int KIND, bool GROUPED>
 __global__ void __launch_bounds__(256, 2)
 masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];   // two K tiles, two V tiles
@@ -226,7 +233,8 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
 #pragma unroll
     for (int i = 0; i < 8; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q + 16 * i));
   }
-  Score<CAP, BIAS> score(a);
+  Score<KIND> score(a);
+  constexpr bool CAP = Score<KIND>::CAP, BIAS = Score<KIND>::BIAS;
   if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
   const int pos = a.row_pos[row];
 
@@ -285,7 +293,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = score.first_reference(), l_run = 0.f;
 
   const std::integral_constant<int, 0> buf0;
   const std::integral_constant<int, 1> buf1;
@@ -307,26 +315,48 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   const unsigned char* const v_rd = lds + 2 * K_TILE + v_lane(lane);
   // Step t multiplies the tile in buffer t % 2 (counted from t_begin), stages tile t + 1, whose rows are in registers, into the other and asks for tile
   // t + 2; past the end of the range its last rows once more, which nobody multiplies.
-  auto tile_step = [&](int t, auto buf) __attribute__((always_inline)) {
+  //
+  // The matrix unit and the vector ALUs run side by side where independent work stands side by side in the instruction stream (a SIMD's two
+  // wavefronts drift into the same phase): the first key block's scores are worked on under the second one's products, the second
+  // one's weights under the products with the first one's.
+  auto tile_step = [&](int t, auto buf, auto whole) __attribute__((always_inline)) {
     constexpr int KOFF = decltype(buf)::value * K_TILE, VOFF = decltype(buf)::value * V_TILE;
+    constexpr bool WHOLE = decltype(whole)::value, EARLY = Score<KIND>::kFixed && WHOLE;   // EARLY: block 0's weights under block 1's products as well
     const std::integral_constant<int, 1 - decltype(buf)::value> other;
     const unsigned row2 = row_of(asked);
     asked = ask(t + 3);
+    if constexpr (BIAS) score.from = (float)(t * BKV + 4 * half - pos);
     f32x16 acc_s[2];
-    {
-      f32x16 zero;
+    auto raw = [&](int b, int e) __attribute__((always_inline)) { acc_s[b][e] = score.raw(acc_s[b][e], (float)(32 * b + 8 * (e >> 2) + (e & 3))); };
+    f32x16 zero;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) zero[e] = 0.f;
-      bf16x8 kf[kAhead];
+    for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+    bf16x8 kf[kAhead], p[4];
+    float sum = 0.f, add = score.add - m_run;   // move_reference's where that moves
+    f32x8 w;
+    auto weight = [&](int b, int j) __attribute__((always_inline)) {
+      w[j & 7] = __builtin_amdgcn_exp2f(fmaf(acc_s[b][j], score.mul, add));
+      sum += w[j & 7];
+      asm volatile("" : "+v"(sum));   // added up here, or the weights stay in registers over the second product
+      if ((j & 7) == 7) p[2 * b + (j >> 3)] = __builtin_convertvector(w, bf16x8);
+    };
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) kf[i] = k_fragment(k_rd + KOFF, i & 1, i >> 1);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < kAhead; ++i) kf[i] = k_fragment(k_rd + KOFF, 0, i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        acc_s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % kAhead], qf[i >> 1], i < 2 ? zero : acc_s[i & 1], 0, 0, 0);
-        if (i + kAhead < 16) kf[i % kAhead] = k_fragment(k_rd + KOFF, (i + kAhead) & 1, (i + kAhead) >> 1);
-        __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < 16; ++i) {
+      const int b = i >> 3;
+      acc_s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % kAhead], qf[i & 7], (i & 7) == 0 ? zero : acc_s[b], 0, 0, 0);
+      if (i + kAhead < 16) kf[i % kAhead] = k_fragment(k_rd + KOFF, (i + kAhead) >> 3, (i + kAhead) & 7);
+      if (i >= 8 && (CAP || BIAS)) {
+        raw(0, 2 * (i - 8));
+        raw(0, 2 * (i - 8) + 1);
+        if constexpr (EARLY) {
+          weight(0, 2 * (i - 8));
+          weight(0, 2 * (i - 8) + 1);
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
     }
     bf16x8 vf[kAhead];
 #pragma unroll
@@ -335,37 +365,42 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     clean_v(t + 1);
     stage_k(other);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (BIAS) score.from = (float)(t * BKV + 4 * half - pos);
+    if constexpr (!EARLY) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int e = 0; e < 16; ++e) raw(1, e);
+      if constexpr (!WHOLE) {
+        const int key0 = t * BKV + 4 * half - mine.lo;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc_s[b][e] = score.raw(acc_s[b][e], (float)(32 * b + 8 * (e >> 2) + (e & 3)));
-    if (t < t_whole || t >= t_ragged) {
-      const int key0 = t * BKV + 4 * half - mine.lo;
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if ((unsigned)(key0 + 32 * b + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[b][e] = score.none();
+          for (int e = 0; e < 16; ++e)
+            if ((unsigned)(key0 + 32 * b + 8 * (e >> 2) + (e & 3)) >= seen) acc_s[b][e] = score.none();
+      }
+      add = move_reference(score, acc_s, m_run, l_run, acc_o);
     }
-    const float add = move_reference(score, acc_s, m_run, l_run, acc_o);
-    bf16x8 p[4];
-    float sum = 0.f;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      p[u] = weights(score, acc_s[u >> 1], u & 1, add, sum);
-      asm volatile("" : "+v"(sum));   // added up here, or the 32 weights stay in registers over the second product
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (!EARLY) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) weight(0, 8 * u + j);
+      }
       __builtin_amdgcn_sched_barrier(0);
-      stage_v(other, u);
+      stage_v(other, 2 * u);
+      stage_v(other, 2 * u + 1);
       __builtin_amdgcn_sched_barrier(0);
     }
-    l_run += sum;
-    __builtin_amdgcn_sched_barrier(0);
     size_t at = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       acc_o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % kAhead], p[i >> 2], acc_o[i & 3], 0, 0, 0);
       if (i + kAhead < 16) vf[i % kAhead] = v_fragment(v_rd + VOFF, (i + kAhead) >> 2, (i + kAhead) & 3);
+      if (i < 8) {
+#pragma unroll
+        for (int j = 2 * i; j < 2 * i + 2; ++j) {
+          if constexpr (EARLY) raw(1, j);
+          weight(1, j);
+        }
+      }
       if (i % 4 == 0) {
         at = row_bytes(row2, i / 4);
         rk[i / 4] = load(k_pool, at);
@@ -373,12 +408,25 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
       if (i % 4 == 2) rv[i / 4] = load(v_pool, at);
       __builtin_amdgcn_sched_barrier(0);
     }
+    l_run += sum;
     __syncthreads();   // tile t consumed, tile t + 1 staged
   };
-  for (int t = t_begin; t < t_end; t += 2) {
-    tile_step(t, buf0);
-    if (t + 1 < t_end) tile_step(t + 1, buf1);
+  const std::true_type whole;
+  const std::false_type part;
+  const int t_lim = min(t_ragged, t_end);
+  int t = t_begin;
+  auto part_tiles = [&](int end) __attribute__((always_inline)) {   // an even number of steps, but at the end of the range
+    for (; t < end; t += 2) {
+      tile_step(t, buf0, part);
+      if (t + 1 < t_end) tile_step(t + 1, buf1, part);
+    }
+  };
+  part_tiles(min(t_whole, t_end));
+  for (; t + 1 < t_lim; t += 2) {
+    tile_step(t, buf0, whole);
+    tile_step(t + 1, buf1, whole);
   }
+  part_tiles(t_end);
   if (bad_v) {
     // whole tiles were not looked at and have multiplied theirs: once more does no harm
     add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, t_begin * BKV, min(t_end * BKV, a.max_len), mine, acc_o);
@@ -411,7 +459,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
 // their own and share nothing before the end.
 static constexpr int kRowWaveBytes = ROW_KEYS * (KROW + VROW);   // a wavefront's K and V, at the end its sums
 static_assert(kRowWaveBytes >= ROW_COLS * PROW * 4, "room for the sums");
-template <bool CAP, bool BIAS>
+template <int KIND>
 __global__ void __launch_bounds__(256, 2)
 masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds_rows[];
@@ -446,7 +494,8 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
 #pragma unroll
     for (int i = 0; i < 8; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q + 16 * i));
   }
-  Score<CAP, BIAS> score(a);
+  Score<KIND> score(a);
+  constexpr bool BIAS = Score<KIND>::BIAS;
   if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
   const int pos = a.row_pos[row];
 
@@ -473,7 +522,7 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc_o[i][e] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = score.first_reference(), l_run = 0.f;
   unsigned char* const k = lds_rows + wave * kRowWaveBytes;
   unsigned char* const v = k + ROW_KEYS * KROW;
   int b = b_begin + wave;
@@ -695,29 +744,29 @@ size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16) {
   return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (PROW + 2);
 }
 
-template <bool CAP, bool BIAS, bool GROUPED>
+template <int KIND, bool GROUPED>
 static hipError_t launch_tiles(const MaskedAttnArgs& a, const MaskedPlan& p, unsigned grid, float* part_o, float2* part_ml, hipStream_t st) {
   static std::atomic<unsigned long long> told{0};
-  const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<CAP, BIAS, GROUPED>, kTileBytes, told);
+  const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<KIND, GROUPED>, kTileBytes, told);
   if (e != hipSuccess) return e;
-  masked_attn_tile_kernel<CAP, BIAS, GROUPED><<<grid, 256, kTileBytes, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
+  masked_attn_tile_kernel<KIND, GROUPED><<<grid, 256, kTileBytes, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
   return hipGetLastError();
 }
 
-template <bool CAP, bool BIAS>
+template <int KIND>
 static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, float* part_o, float2* part_ml, hipStream_t st) {
   const long grid = (long)p.slots * p.split.n_chunks * a.g.n_kv_heads;
   if (grid > INT_MAX) return hipErrorInvalidValue;
   if (p.rows) {
     static std::atomic<unsigned long long> told{0};
-    const hipError_t e = allow_dynamic_lds((const void*)masked_attn_rows_kernel<CAP, BIAS>, 4 * kRowWaveBytes, told);
+    const hipError_t e = allow_dynamic_lds((const void*)masked_attn_rows_kernel<KIND>, 4 * kRowWaveBytes, told);
     if (e != hipSuccess) return e;
-    masked_attn_rows_kernel<CAP, BIAS><<<(unsigned)grid, 256, 4 * kRowWaveBytes, st>>>(a, p.split, part_o, part_ml);
+    masked_attn_rows_kernel<KIND><<<(unsigned)grid, 256, 4 * kRowWaveBytes, st>>>(a, p.split, part_o, part_ml);
   } else {
     // pages of 16, 32, 64, ... slots, or one block a sequence whose slots are a multiple of 16
     const bool grouped = a.g.max_blocks == 1 ? a.g.block_size % 16 == 0 : a.g.bs_shift >= 4;
-    return grouped ? launch_tiles<CAP, BIAS, true>(a, p, (unsigned)grid, part_o, part_ml, st)
-                   : launch_tiles<CAP, BIAS, false>(a, p, (unsigned)grid, part_o, part_ml, st);
+    return grouped ? launch_tiles<KIND, true>(a, p, (unsigned)grid, part_o, part_ml, st)
+                   : launch_tiles<KIND, false>(a, p, (unsigned)grid, part_o, part_ml, st);
   }
   return hipGetLastError();
 }
@@ -732,8 +781,12 @@ hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float*
   if (!part) p.split = {1, 0};
   float2* const part_ml = reinterpret_cast<float2*>(part + (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * PROW);
   const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
-  const hipError_t e = cap ? (bias ? launch_bf16<true, true>(a, p, part, part_ml, st) : launch_bf16<true, false>(a, p, part, part_ml, st))
-                           : (bias ? launch_bf16<false, true>(a, p, part, part_ml, st) : launch_bf16<false, false>(a, p, part, part_ml, st));
+  hipError_t e;
+  if (cap && bias) e = launch_bf16<kCapBias>(a, p, part, part_ml, st);
+  else if (bias) e = launch_bf16<kBias>(a, p, part, part_ml, st);
+  else if (!cap) e = launch_bf16<kPlain>(a, p, part, part_ml, st);
+  else if (a.cap * kLog2e <= kMostBounded) e = launch_bf16<kBounded>(a, p, part, part_ml, st);
+  else e = launch_bf16<kCap>(a, p, part, part_ml, st);
   if (e != hipSuccess || p.split.n_chunks <= 1) return e;
   masked_attn_merge_kernel<<<per_row, 256, 0, st>>>(a, p.split, p.cols, p.rows_per_tile, part, part_ml);
   return hipGetLastError();
