@@ -472,6 +472,18 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
   const int n_cols = (sq.r1 - sq.r0) * G;   // at most 32 (host)
   if (n_cols <= 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+  // the blocks of the first keys, beside the rows' ranges, for ranges that begin with the chunk
+  const bool is_split = sp.n_chunks > 1;
+  const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
+  const int max_key = a.max_len - 1, last_block = a.g.max_blocks - 1, block_size = a.g.block_size;
+  const KvGeom geom = a.g;
+  struct Asked { int block, slot; };
+  auto ask = [&](int b) __attribute__((always_inline)) -> Asked {
+    const int key = min(b * ROW_KEYS + col, max_key), at = block_of(geom, key);
+    return {table[min(at, last_block)], key - at * block_size};
+  };
+  const int b_chunk = chunk * (sp.chunk / ROW_KEYS);
+  Asked q0 = ask(b_chunk + wave), next = ask(b_chunk + wave + 4);
   const int row = sq.r0 + min(col, n_cols - 1) / G, head = kvh * G + min(col, n_cols - 1) % G;
   const Range mine = range_of_row(a, row);
   const unsigned seen = mine.hi < 0 ? 0u : (unsigned)(mine.hi - mine.lo) + 1u;
@@ -483,7 +495,6 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
   }
   lo_min = __builtin_amdgcn_readfirstlane(lo_min); lo_max = __builtin_amdgcn_readfirstlane(lo_max);
   hi_min = __builtin_amdgcn_readfirstlane(hi_min); hi_max = __builtin_amdgcn_readfirstlane(hi_max);
-  const bool is_split = sp.n_chunks > 1;
   const int key_end = is_split ? min(hi_max + 1, (chunk + 1) * sp.chunk) : hi_max + 1;
   const int b_begin = hi_max < 0 ? 0 : max(lo_min, chunk * sp.chunk) / ROW_KEYS, b_end = (key_end + ROW_KEYS - 1) / ROW_KEYS;
   if (b_begin >= b_end && is_split) return;
@@ -499,15 +510,9 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
   if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
   const int pos = a.row_pos[row];
 
-  const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
-  struct Asked { int block, slot; };
-  auto ask = [&](int b) __attribute__((always_inline)) -> Asked {
-    const int key = min(min(b, b_end - 1) * ROW_KEYS + col, a.max_len - 1), at = block_of(a.g, key);
-    return {table[min(at, a.g.max_blocks - 1)], key - at * a.g.block_size};
-  };
   u32x4 rk[8], rv[8];
   auto fetch = [&](Asked q) __attribute__((always_inline)) {
-    const unsigned pool_row = (unsigned)(min(max(q.block, 0), a.g.n_blocks - 1) * a.g.n_kv_heads + kvh) * (unsigned)a.g.block_size + q.slot;
+    const unsigned pool_row = (unsigned)(min(max(q.block, 0), geom.n_blocks - 1) * geom.n_kv_heads + kvh) * (unsigned)block_size + q.slot;
     size_t off[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) off[i] = (size_t)(unsigned)__shfl((int)pool_row, 4 * i + (lane >> 4), 64) * 256 + (lane & 15) * 16;
@@ -528,9 +533,11 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
   int b = b_begin + wave;
   bool bad = false;
   if (b < b_end) {
-    Asked next = ask(b);
-    fetch(next);
-    next = ask(b + 4);
+    if (b_begin != b_chunk) {   // uniform
+      q0 = ask(b);
+      next = ask(b + 4);
+    }
+    fetch(q0);
     for (; b < b_end; b += 4) {
       const bool whole = b * ROW_KEYS >= lo_max && b * ROW_KEYS + ROW_KEYS - 1 <= hi_min;
       if (!whole) {
@@ -626,45 +633,75 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
 }
 
 // ------------------------------------------------------------------ merge of the chunks
-// A wavefront per (row, head), 32 lanes with four elements each of every other chunk.  A chunk left a result for a column
-// exactly if the tile's range reaches into it, which it does where the row's own range does.
+// A wavefront per (row, head); lane c has chunk c's exponent and sum, 32 lanes with four elements each read the outputs of every other chunk.  A
+// chunk left a result for a column exactly if the tile's range reaches into it, which it does where the row's own range does.
+// Bound by a chain of dependent reads.  ROWS (results of the few-row kernel): what is read does not hang on the rows' places, so
+// that the results of the first chunks are asked for beside the row's range.
+static constexpr int kMaxChunks = 64;   // a lane each
+template <bool ROWS>
 __global__ void __launch_bounds__(256)
-masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int cols, int rows_per_tile, const float* __restrict__ part_o,
-                         const float2* __restrict__ part_ml) {
+masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, const float* __restrict__ part_o, const float2* __restrict__ part_ml) {
   const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = (int)(item / a.n_q_heads), head = (int)(item - (long)row * a.n_q_heads);
-  if (row >= a.n_rows) return;
+  const int row_or = (int)(item / a.n_q_heads), head = (int)(item - (long)row_or * a.n_q_heads);   // ROWS: row in_seq of sequence s, in turn
   const int lane = threadIdx.x & 63, d = (lane & 31) * 4, odd = lane >> 5;
   const int G = a.n_q_heads / a.g.n_kv_heads, kvh = head / G;
-  const int s = last_at_or_before(a.n_seq, row, [&](int i) { return min(max(a.row_start[i], 0), a.n_rows); });
+  int s, in_seq, row;
+  if constexpr (ROWS) {
+    s = row_or / a.max_rows_per_seq;
+    in_seq = row_or - s * a.max_rows_per_seq;
+    if (s >= a.n_seq) return;
+  } else {
+    row = row_or;
+    if (row >= a.n_rows) return;
+    s = last_at_or_before(a.n_seq, row, [&](int i) { return min(max(a.row_start[i], 0), a.n_rows); });
+  }
   const SeqRows sq = rows_of_seq(a, s);
-  if (row < sq.r0 || row >= sq.r1) return;
+  if constexpr (!ROWS) {
+    if (row < sq.r0 || row >= sq.r1) return;
+    in_seq = row - sq.r0;
+  }
+  constexpr int cols = ROWS ? ROW_COLS : TILE_COLS;
+  const long slot = ROWS ? s : sq.r0 / rows_per_tile + s + in_seq / rows_per_tile;
+  const int col = (ROWS ? in_seq : in_seq % rows_per_tile) * G + head - kvh * G;
+  const size_t first = ((size_t)slot * sp.n_chunks * a.g.n_kv_heads + kvh) * cols + col, step = (size_t)a.g.n_kv_heads * cols;
+  const float2 ml = part_ml[first + min(lane, sp.n_chunks - 1) * step];
+  float4 o[4];
+  auto fetch = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = *reinterpret_cast<const float4*>(part_o + (first + min(c + 2 * i + odd, sp.n_chunks - 1) * step) * PROW + d);
+  };
+  if constexpr (ROWS) {
+    fetch(0);
+    row = sq.r0 + in_seq;
+    if (row >= sq.r1) return;
+  }
   const Range r = range_of_row(a, row);
   bf16* const out = reinterpret_cast<bf16*>(a.out) + ((size_t)row * a.n_q_heads + head) * DH + d;
   if (r.hi < 0) {
     if (!odd) *reinterpret_cast<uint2*>(out) = make_uint2(0u, 0u);
     return;
   }
-  const int in_seq = row - sq.r0;
-  const long slot = cols == ROW_COLS ? s : sq.r0 / rows_per_tile + s + in_seq / rows_per_tile;
-  const int col = (cols == ROW_COLS ? in_seq : in_seq % rows_per_tile) * G + head - kvh * G;
   const int c0 = r.lo / sp.chunk, c1 = r.hi / sp.chunk;
-  auto at = [&](int c) { return ((size_t)(slot * sp.n_chunks + c) * a.g.n_kv_heads + kvh) * cols + col; };
-  float m = -INFINITY;
-  for (int c = c0 + lane; c <= c1; c += 64) m = fmaxf(m, part_ml[at(c)].x);
+  const bool mine = lane >= c0 && lane <= c1 && ml.x != -INFINITY;
+  float m = mine ? ml.x : -INFINITY;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-  float l = 0.f;
+  for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k, 64));
+  const float w = mine ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
+  float l = mine ? ml.y * w : 0.f;
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) l += __shfl_xor(l, k, 64);
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = c0 + odd; c <= c1; c += 2) {
-    const float2 x = part_ml[at(c)];
-    if (x.x == -INFINITY) continue;
-    const float w = __builtin_amdgcn_exp2f(x.x - m);
-    const float4 o = *reinterpret_cast<const float4*>(part_o + at(c) * PROW + d);
-    l += x.y * w;
-    acc.x += o.x * w; acc.y += o.y * w; acc.z += o.z * w; acc.w += o.w * w;
+  const int from = ROWS ? 0 : c0 & ~7;
+  for (int c = from; c <= c1; c += 8) {
+    if (!ROWS || c > 0) fetch(c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int at = c + 2 * i + odd;
+      const float by = __shfl(w, at & 63, 64);
+      // not a factor of 0: what lies there may be no number
+      if (at <= c1 && by > 0.f) { acc.x += o[i].x * by; acc.y += o[i].y * by; acc.z += o[i].z * by; acc.w += o[i].w * by; }
+    }
   }
-  l += __shfl_xor(l, 32, 64);
   acc.x += __shfl_xor(acc.x, 32, 64); acc.y += __shfl_xor(acc.y, 32, 64); acc.z += __shfl_xor(acc.z, 32, 64); acc.w += __shfl_xor(acc.w, 32, 64);
   const float inv = 1.0f / l;
   if (!odd) *reinterpret_cast<uint2*>(out) = pack4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
@@ -720,6 +757,10 @@ masked_attn_f32_kernel(MaskedAttnArgs a) {
 
 // ------------------------------------------------------------------ host
 // The few-row kernel serves sequences whose columns fit 32; the grid is then (sequence, chunk), else (tile, chunk).
+// Key ranges are cut until there are as many workgroups as compute units (tiles: as run at a time, two on each), but into chunks of 256 (512) keys at
+// least: more and shorter ones cost more in the merge and in beginnings than they spread.  A token for each of 8 sequences of 16k keys: 110 us
+// with 256 workgroups wanted, 111 with 1024, 125 with 4096; of one sequence of 40k keys 44 and 48; of one of 5k keys 16.0 in chunks of 256,
+// 18.5 in chunks of 128.
 struct MaskedPlan { bool rows; int slots, rows_per_tile, cols; MaskedSplit split; };
 static MaskedPlan plan_masked(const MaskedAttnArgs& a) {
   MaskedPlan p;
@@ -729,8 +770,8 @@ static MaskedPlan plan_masked(const MaskedAttnArgs& a) {
   p.rows_per_tile = TILE_COLS / G;
   p.slots = p.rows ? a.n_seq : a.n_rows / p.rows_per_tile + a.n_seq;
   const long wgs = (long)p.slots * a.g.n_kv_heads;
-  const long unit = p.rows ? 4 * ROW_KEYS : BKV, least = p.rows ? 256 : 512, wanted = 1024;
-  long chunks = std::min(wanted / std::max(wgs, 1l), (a.max_len + least - 1) / least);
+  const long unit = p.rows ? 4 * ROW_KEYS : BKV, least = p.rows ? 256 : 512, wanted = p.rows ? 256 : 512;
+  long chunks = std::min({wanted / std::max(wgs, 1l), (a.max_len + least - 1) / least, (long)kMaxChunks});
   long chunk = chunks <= 1 ? 0 : ((a.max_len + chunks - 1) / chunks + unit - 1) / unit * unit;
   p.split.n_chunks = chunk ? (int)((a.max_len + chunk - 1) / chunk) : 1;
   p.split.chunk = (int)chunk;
@@ -788,7 +829,12 @@ hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float*
   else if (a.cap * kLog2e <= kMostBounded) e = launch_bf16<kBounded>(a, p, part, part_ml, st);
   else e = launch_bf16<kCap>(a, p, part, part_ml, st);
   if (e != hipSuccess || p.split.n_chunks <= 1) return e;
-  masked_attn_merge_kernel<<<per_row, 256, 0, st>>>(a, p.split, p.cols, p.rows_per_tile, part, part_ml);
+  if (p.rows) {
+    const unsigned grid = (unsigned)(((long)a.n_seq * a.max_rows_per_seq * a.n_q_heads + 3) / 4);
+    masked_attn_merge_kernel<true><<<grid, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
+  } else {
+    masked_attn_merge_kernel<false><<<per_row, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
+  }
   return hipGetLastError();
 }
 
