@@ -27,6 +27,7 @@ static constexpr int DH = 128;
 static constexpr int BKV = 64;            // keys per tile of the tile kernel
 static constexpr int TILE_COLS = 128;     // columns of a tile: four wavefronts, 32 each
 static constexpr int ROW_COLS = 32;       // columns of the few-row kernel
+static constexpr int F32_COLS = 16;       // columns of the float kernel
 static constexpr int ROW_KEYS = 32;       // keys a wavefront of it takes at a time
 static constexpr int KROW = DH * 2 + 16, VROW = DH * 2 + 64;   // bytes between rows in LDS
 static constexpr int PROW = DH + 4;       // floats between the columns of a partial result
@@ -178,12 +179,16 @@ __device__ __forceinline__ bf16x8 v_fragment(const unsigned char* v, int t, int 
   return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(at(16 * t), at(16 * t + 8), 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+__device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
+
 // how a batch's key ranges are cut
 struct MaskedSplit { int n_chunks, chunk; };   // chunk: keys
 
 __device__ inline uint2 pack4(float a, float b, float c, float d) {
   return make_uint2((uint32_t)f32_to_bf16(a).v | ((uint32_t)f32_to_bf16(b).v << 16), (uint32_t)f32_to_bf16(c).v | ((uint32_t)f32_to_bf16(d).v << 16));
 }
+
+__device__ inline void store4(bf16* p, float a, float b, float c, float d) { *reinterpret_cast<uint2*>(p) = pack4(a, b, c, d); }
 
 // ------------------------------------------------------------------ tiles of 128 columns
 // Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
@@ -633,17 +638,18 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
 }
 
 // ------------------------------------------------------------------ merge of the chunks
-// A wavefront per (row, head); lane c has chunk c's exponent and sum, 32 lanes with four elements each read the outputs of every other chunk.  A
-// chunk left a result for a column exactly if the tile's range reaches into it, which it does where the row's own range does.
+// A wavefront per (row, head); lane c has chunk c's exponent and sum, D / 4 lanes with four elements each read the outputs of every second (fourth)
+// chunk.  A chunk left a result for a column exactly if the tile's range reaches into it, which it does where the row's own range does.
 // Bound by a chain of dependent reads.  ROWS (results of the few-row kernel): what is read does not hang on the rows' places, so
 // that the results of the first chunks are asked for beside the row's range.
 static constexpr int kMaxChunks = 64;   // a lane each
-template <bool ROWS>
+template <typename T, int D, int COLS, bool ROWS>
 __global__ void __launch_bounds__(256)
 masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, const float* __restrict__ part_o, const float2* __restrict__ part_ml) {
   const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int row_or = (int)(item / a.n_q_heads), head = (int)(item - (long)row_or * a.n_q_heads);   // ROWS: row in_seq of sequence s, in turn
-  const int lane = threadIdx.x & 63, d = (lane & 31) * 4, odd = lane >> 5;
+  constexpr int LANES = D / 4, TURNS = 64 / LANES;   // of a chunk; chunks side by side
+  const int lane = threadIdx.x & 63, d = (lane % LANES) * 4, turn = lane / LANES;
   const int G = a.n_q_heads / a.g.n_kv_heads, kvh = head / G;
   int s, in_seq, row;
   if constexpr (ROWS) {
@@ -660,15 +666,18 @@ masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, co
     if (row < sq.r0 || row >= sq.r1) return;
     in_seq = row - sq.r0;
   }
-  constexpr int cols = ROWS ? ROW_COLS : TILE_COLS;
-  const long slot = ROWS ? s : sq.r0 / rows_per_tile + s + in_seq / rows_per_tile;
-  const int col = (ROWS ? in_seq : in_seq % rows_per_tile) * G + head - kvh * G;
-  const size_t first = ((size_t)slot * sp.n_chunks * a.g.n_kv_heads + kvh) * cols + col, step = (size_t)a.g.n_kv_heads * cols;
+  const int h = head - kvh * G;
+  long slot;
+  int col;
+  if constexpr (ROWS) { slot = s; col = in_seq * G + h; }
+  else if constexpr (COLS == F32_COLS) { const long c = (long)in_seq * G + h; slot = (long)sq.r0 * G / COLS + s + c / COLS; col = (int)(c % COLS); }
+  else { slot = sq.r0 / rows_per_tile + s + in_seq / rows_per_tile; col = in_seq % rows_per_tile * G + h; }
+  const size_t first = ((size_t)slot * sp.n_chunks * a.g.n_kv_heads + kvh) * COLS + col, step = (size_t)a.g.n_kv_heads * COLS;
   const float2 ml = part_ml[first + min(lane, sp.n_chunks - 1) * step];
   float4 o[4];
   auto fetch = [&](int c) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = *reinterpret_cast<const float4*>(part_o + (first + min(c + 2 * i + odd, sp.n_chunks - 1) * step) * PROW + d);
+    for (int i = 0; i < 4; ++i) o[i] = *reinterpret_cast<const float4*>(part_o + (first + min(c + TURNS * i + turn, sp.n_chunks - 1) * step) * (D + 4) + d);
   };
   if constexpr (ROWS) {
     fetch(0);
@@ -676,9 +685,9 @@ masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, co
     if (row >= sq.r1) return;
   }
   const Range r = range_of_row(a, row);
-  bf16* const out = reinterpret_cast<bf16*>(a.out) + ((size_t)row * a.n_q_heads + head) * DH + d;
+  T* const out = reinterpret_cast<T*>(a.out) + ((size_t)row * a.n_q_heads + head) * D + d;
   if (r.hi < 0) {
-    if (!odd) *reinterpret_cast<uint2*>(out) = make_uint2(0u, 0u);
+    if (turn == 0) store4(out, 0.f, 0.f, 0.f, 0.f);
     return;
   }
   const int c0 = r.lo / sp.chunk, c1 = r.hi / sp.chunk;
@@ -691,98 +700,237 @@ masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, co
 #pragma unroll
   for (int k = 32; k > 0; k >>= 1) l += __shfl_xor(l, k, 64);
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  const int from = ROWS ? 0 : c0 & ~7;
-  for (int c = from; c <= c1; c += 8) {
+  const int from = ROWS ? 0 : c0;
+  for (int c = from; c <= c1; c += 4 * TURNS) {
     if (!ROWS || c > 0) fetch(c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int at = c + 2 * i + odd;
+      const int at = c + TURNS * i + turn;
       const float by = __shfl(w, at & 63, 64);
       // not a factor of 0: what lies there may be no number
       if (at <= c1 && by > 0.f) { acc.x += o[i].x * by; acc.y += o[i].y * by; acc.z += o[i].z * by; acc.w += o[i].w * by; }
     }
   }
-  acc.x += __shfl_xor(acc.x, 32, 64); acc.y += __shfl_xor(acc.y, 32, 64); acc.z += __shfl_xor(acc.z, 32, 64); acc.w += __shfl_xor(acc.w, 32, 64);
+#pragma unroll
+  for (int k = 32; k >= LANES; k >>= 1) { acc.x += __shfl_xor(acc.x, k, 64); acc.y += __shfl_xor(acc.y, k, 64); acc.z += __shfl_xor(acc.z, k, 64); acc.w += __shfl_xor(acc.w, k, 64); }
   const float inv = 1.0f / l;
-  if (!odd) *reinterpret_cast<uint2*>(out) = pack4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+  if (turn == 0) store4(out, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
 }
 
-// ------------------------------------------------------------------ float: one wavefront per (row, head)
-// 64 keys at a time, a lane a key for the scores, an element or two of the head a lane for the values.
-__global__ void __launch_bounds__(256)
-masked_attn_f32_kernel(MaskedAttnArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long item = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = (int)(item / a.n_q_heads), head = (int)(item - (long)row * a.n_q_heads);
-  if (row >= a.n_rows) return;
-  const int s = last_at_or_before(a.n_seq, row, [&](int i) { return min(max(a.row_start[i], 0), a.n_rows); });
+// ------------------------------------------------------------------ float
+// 16 columns a workgroup on 16x16x4 matrix instructions; its wavefronts take every eighth (heads of 128: fourth) block of 16 keys of the range with a
+// softmax of their own and are merged through LDS.  Bound by latency (float models have a few hundred keys), so K and V go from memory straight to
+// registers, the next block's keys under the softmax and its values under the scores.
+//   S^T[key][column]: lane holds column lane % 16, keys 4 (lane / 16) + 0..3; O^T[d][column] += V^T[d][key] P: P's operand is S^T's result as it stands
+// The tanh is the library's: what the quotient of the bf16 kernels loses (2^-23 of the cap) shows in a float output.
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
+template <int D>
+__global__ void __launch_bounds__(D == 64 ? 512 : 256, 2)
+masked_attn_f32_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, float* __restrict__ part_o, float2* __restrict__ part_ml) {
+  constexpr int NB = D / 16, NW = D == 64 ? 8 : 4, OROW = D + 4;
+  __shared__ __attribute__((aligned(16))) float lds_o[NW][F32_COLS][OROW];
+  __shared__ float2 lds_ml[NW][F32_COLS];
+  const int kvh = (int)blockIdx.x % a.g.n_kv_heads;
+  const int item = (int)blockIdx.x / a.g.n_kv_heads;
+  const int slot = n_slots - 1 - item / sp.n_chunks, chunk = item % sp.n_chunks;
+  const int G = a.n_q_heads / a.g.n_kv_heads;
+  const int s = last_at_or_before(a.n_seq, slot, [&](int i) { return (int)((long)min(max(a.row_start[i], 0), a.n_rows) * G / F32_COLS) + i; });
   const SeqRows sq = rows_of_seq(a, s);
-  if (row < sq.r0 || row >= sq.r1) return;
-  const int dh = a.g.head_dim, kvh = head / (a.n_q_heads / a.g.n_kv_heads);
-  const int pos = a.row_pos[row];
-  const Range r = range_of_row(a, row);
-  const float* const q = reinterpret_cast<const float*>(a.q) + ((size_t)row * a.n_q_heads + head) * dh;
+  const long first = (long)(slot - ((int)((long)sq.r0 * G / F32_COLS) + s)) * F32_COLS;
+  const int n_valid = (int)min((long)F32_COLS, (long)(sq.r1 - sq.r0) * G - first);
+  if (n_valid <= 0 || first < 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), qi = lane & 15, kq = lane >> 4;
+  const long col = first + min(qi, n_valid - 1);
+  const int row = sq.r0 + (int)(col / G), head = kvh * G + (int)(col % G);
+  const Range mine = range_of_row(a, row);
+  const unsigned seen = mine.hi < 0 ? 0u : (unsigned)(mine.hi - mine.lo) + 1u;
+  int lo_min = mine.lo, lo_max = mine.lo, hi_min = mine.hi, hi_max = mine.hi;
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    lo_min = min(lo_min, __shfl_xor(lo_min, o, 64)); lo_max = max(lo_max, __shfl_xor(lo_max, o, 64));
+    hi_min = min(hi_min, __shfl_xor(hi_min, o, 64)); hi_max = max(hi_max, __shfl_xor(hi_max, o, 64));
+  }
+  lo_min = __builtin_amdgcn_readfirstlane(lo_min); lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+  hi_min = __builtin_amdgcn_readfirstlane(hi_min); hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+  const bool is_split = sp.n_chunks > 1;
+  const int key_end = is_split ? min(hi_max + 1, (chunk + 1) * sp.chunk) : hi_max + 1;
+  const int b_begin = hi_max < 0 ? 0 : max(lo_min, chunk * sp.chunk) / 16, b_end = (key_end + 15) / 16;
+  if (b_begin >= b_end && is_split) return;
+
+  const float* const q = reinterpret_cast<const float*>(a.q) + ((size_t)row * a.n_q_heads + head) * D + 4 * kq;
+  f32x4 fq[NB], fk[NB], acc[NB], fv[NB];   // fv[t][c]: V[key 4 kq + c][16 t + qi]
+#pragma unroll
+  for (int t = 0; t < NB; ++t) {
+    fq[t] = *reinterpret_cast<const f32x4*>(q + 16 * t);
+    acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   const float slope = a.slopes ? a.slopes[head] : 0.f;
-  float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-  for (long k0 = r.lo; k0 <= r.hi; k0 += 64) {
-    const int key = (int)min(k0 + lane, (long)r.hi);
-    const float* const k = reinterpret_cast<const float*>(a.k_pool) + kv_row_offset(a.g, sq.table_row, key, kvh);
-    float x = 0.f;
-    for (int d = 0; d < dh; ++d) x += q[d] * k[d];
-    x *= a.scale;
-    if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
-    x -= slope * fabsf((float)(pos - key));
-    if (k0 + lane > r.hi) x = -INFINITY;
-    float mx = x;
-    for (int w = 32; w > 0; w >>= 1) mx = fmaxf(mx, __shfl_xor(mx, w, 64));
-    const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float corr = __expf(m - m_use), p = k0 + lane > r.hi ? 0.f : __expf(x - m_use);
-    m = m_new;
-    l = l * corr + p;
-    o0 *= corr;
-    o1 *= corr;
-    for (int j = 0; j < (int)min(64l, r.hi - k0 + 1); ++j) {
-      const float w = __shfl(p, j, 64);
-      const float* const v = reinterpret_cast<const float*>(a.v_pool) + kv_row_offset(a.g, sq.table_row, (int)k0 + j, kvh);
-      o0 += w * v[lane];
-      if (dh == 128) o1 += w * v[lane + 64];
+  const int pos = a.row_pos[row];
+  const float* const k_pool = reinterpret_cast<const float*>(a.k_pool);
+  const float* const v_pool = reinterpret_cast<const float*>(a.v_pool);
+  const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
+  const KvGeom geom = a.g;
+  const int max_key = a.max_len - 1;
+  auto ask = [&](int b) __attribute__((always_inline)) -> int {   // the pool row of key qi of a block
+    const int key = min(min(b, b_end - 1) * 16 + qi, max_key), at = block_of(geom, key);
+    return (min(max(table[min(at, geom.max_blocks - 1)], 0), geom.n_blocks - 1) * geom.n_kv_heads + kvh) * geom.block_size + (key - at * geom.block_size);
+  };
+  auto load_k = [&](int pool_row) __attribute__((always_inline)) {
+    const float* const p = k_pool + (size_t)(unsigned)pool_row * D + 4 * kq;
+#pragma unroll
+    for (int t = 0; t < NB; ++t) fk[t] = *reinterpret_cast<const f32x4*>(p + 16 * t);
+  };
+  auto load_v = [&](int pool_row) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float* const p = v_pool + (size_t)(unsigned)__shfl(pool_row, 4 * kq + c, 64) * D + qi;
+#pragma unroll
+      for (int t = 0; t < NB; ++t) fv[t][c] = p[16 * t];
+    }
+  };
+  float m_run = -INFINITY, l_run = 0.f;
+  bool bad = false;
+  int b = b_begin + wave;
+  if (b < b_end) {
+    int at = ask(b), next = ask(b + NW);
+    load_k(at);
+    load_v(at);
+    for (; b < b_end; b += NW) {
+      const bool whole = b * 16 >= lo_max && b * 16 + 15 <= hi_min;
+      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;
+#pragma unroll
+      for (int t = 0; t < NB; t += 2)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(fk[t][c], fq[t][c], s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(fk[t + 1][c], fq[t + 1][c], s1, 0, 0, 0);
+        }
+      load_k(next);   // behind the range its last block once more
+      float x[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[r] = (s0[r] + s1[r]) * a.scale;
+        if (a.cap > 0.f) x[r] = a.cap * tanhf(x[r] / a.cap);
+        x[r] = fmaf(-slope, fabsf((float)(b * 16 + 4 * kq + r - pos)), x[r]);
+      }
+      if (!whole) {
+        const int key0 = b * 16 + 4 * kq - mine.lo;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if ((unsigned)(key0 + r) >= seen) x[r] = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < NB; ++t)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            if (!(fabsf(fv[t][c]) < INFINITY)) { fv[t][c] = 0.f; bad = true; }
+      }
+      float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * kLog2e;
+      const float m_new = fmaxf(m_run, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+      if (__any(m_new > m_run)) {
+        const float corr = __builtin_amdgcn_exp2f(m_run - m_use);
+        l_run *= corr;
+#pragma unroll
+        for (int t = 0; t < NB; ++t) acc[t] *= corr;
+        m_run = m_new;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        x[r] = __builtin_amdgcn_exp2f(fmaf(x[r], kLog2e, -m_use));
+        l_run += x[r];
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int t = 0; t < NB; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fv[t][c], x[c], acc[t], 0, 0, 0);
+      load_v(next);
+      next = ask(b + 2 * NW);
+    }
+    if (__any(bad)) {
+      for (b = b_begin + wave; b < b_end; b += NW)
+        for (int key = b * 16; key < min(b * 16 + 16, a.max_len); ++key) {
+          const bool sees = mine.lo <= key && key <= mine.hi;
+          const float* const v = v_pool + kv_row_offset(geom, sq.table_row, key, kvh) + 4 * kq;
+#pragma unroll
+          for (int t = 0; t < NB; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float y = v[16 * t + r];
+              if (sees && !(fabsf(y) < INFINITY)) acc[t][r] += y;
+            }
+        }
     }
   }
-  for (int w = 32; w > 0; w >>= 1) l += __shfl_xor(l, w, 64);
-  float* const out = reinterpret_cast<float*>(a.out) + ((size_t)row * a.n_q_heads + head) * dh;
-  const float inv = r.hi < 0 ? 0.f : 1.f / l;
-  out[lane] = o0 * inv;
-  if (dh == 128) out[lane + 64] = o1 * inv;
+
+  // the wavefronts' sums, in their order
+  float l_tot = l_run + __shfl_xor(l_run, 16, 64);
+  l_tot += __shfl_xor(l_tot, 32, 64);
+  if (kq == 0) lds_ml[wave][qi] = make_float2(m_run, l_tot);
+  __syncthreads();
+  float m_all = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) m_all = fmaxf(m_all, lds_ml[w][qi].x);
+  const float by = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m_all);
+#pragma unroll
+  for (int t = 0; t < NB; ++t) {
+    const f32x4 o = by == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[t] * by;
+    *reinterpret_cast<f32x4*>(&lds_o[wave][qi][16 * t + 4 * kq]) = o;
+  }
+  __syncthreads();
+  for (int i = tid; i < n_valid * (D / 4); i += NW * 64) {
+    const int c = i / (D / 4), d = (i - c * (D / 4)) * 4;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, lds_ml[w][c].x);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      o += *reinterpret_cast<const f32x4*>(&lds_o[w][c][d]);
+      l += lds_ml[w][c].x == -INFINITY ? 0.f : lds_ml[w][c].y * __builtin_amdgcn_exp2f(lds_ml[w][c].x - m);
+    }
+    if (is_split) {
+      const size_t to = ((size_t)((long)slot * sp.n_chunks + chunk) * a.g.n_kv_heads + kvh) * F32_COLS + c;
+      if (d == 0) part_ml[to] = make_float2(m, l);
+      store4(part_o + to * OROW + d, o[0], o[1], o[2], o[3]);
+    } else {
+      const long cc = first + c;
+      const int r = sq.r0 + (int)(cc / G), h = kvh * G + (int)(cc % G);
+      const float inv = range_of_row(a, r).hi < 0 ? 0.f : 1.0f / l;
+      store4(reinterpret_cast<float*>(a.out) + ((size_t)r * a.n_q_heads + h) * D + d, o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv);
+    }
+  }
 }
 
 // ------------------------------------------------------------------ host
 // The few-row kernel serves sequences whose columns fit 32; the grid is then (sequence, chunk), else (tile, chunk).
-// Key ranges are cut until there are as many workgroups as compute units (tiles: as run at a time, two on each), but into chunks of 256 (512) keys at
-// least: more and shorter ones cost more in the merge and in beginnings than they spread.  A token for each of 8 sequences of 16k keys: 110 us
+// Key ranges are cut until there are as many workgroups as compute units (tiles: as run at a time, two on each), but into chunks of 256 keys at
+// least (tiles: 512; float: eight steps of a workgroup, which the merge's launch costs): more and shorter ones cost more in the merge and in beginnings than they spread.  A token for each of 8 sequences of 16k keys: 110 us
 // with 256 workgroups wanted, 111 with 1024, 125 with 4096; of one sequence of 40k keys 44 and 48; of one of 5k keys 16.0 in chunks of 256,
 // 18.5 in chunks of 128.
-struct MaskedPlan { bool rows; int slots, rows_per_tile, cols; MaskedSplit split; };
-static MaskedPlan plan_masked(const MaskedAttnArgs& a) {
+struct MaskedPlan { bool rows; long slots; int rows_per_tile, cols; MaskedSplit split; };
+static MaskedPlan plan_masked(const MaskedAttnArgs& a, bool is_bf16) {
   MaskedPlan p;
   const int G = a.n_q_heads / a.g.n_kv_heads;
-  p.rows = (long)a.max_rows_per_seq * G <= ROW_COLS;
-  p.cols = p.rows ? ROW_COLS : TILE_COLS;
+  p.rows = is_bf16 && (long)a.max_rows_per_seq * G <= ROW_COLS;
+  p.cols = !is_bf16 ? F32_COLS : p.rows ? ROW_COLS : TILE_COLS;
   p.rows_per_tile = TILE_COLS / G;
-  p.slots = p.rows ? a.n_seq : a.n_rows / p.rows_per_tile + a.n_seq;
-  const long wgs = (long)p.slots * a.g.n_kv_heads;
-  const long unit = p.rows ? 4 * ROW_KEYS : BKV, least = p.rows ? 256 : 512, wanted = p.rows ? 256 : 512;
-  long chunks = std::min({wanted / std::max(wgs, 1l), (a.max_len + least - 1) / least, (long)kMaxChunks});
-  long chunk = chunks <= 1 ? 0 : ((a.max_len + chunks - 1) / chunks + unit - 1) / unit * unit;
+  p.slots = !is_bf16 ? (long)a.n_rows * G / F32_COLS + a.n_seq : p.rows ? a.n_seq : a.n_rows / p.rows_per_tile + a.n_seq;
+  const bool tiles = is_bf16 && !p.rows;
+  const long wgs = p.slots * a.g.n_kv_heads;
+  const long unit = tiles ? BKV : 128, least = !is_bf16 ? (a.g.head_dim == 64 ? 1024 : 512) : tiles ? 512 : 256, wanted = tiles ? 512 : 256;
+  const long chunks = std::min({wanted / std::max(wgs, 1l), (a.max_len + least - 1) / least, (long)kMaxChunks});
+  const long chunk = chunks <= 1 ? 0 : ((a.max_len + chunks - 1) / chunks + unit - 1) / unit * unit;
   p.split.n_chunks = chunk ? (int)((a.max_len + chunk - 1) / chunk) : 1;
   p.split.chunk = (int)chunk;
   return p;
 }
 
 size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16) {
-  if (!is_bf16 || a.n_rows <= 0) return 0;
-  const MaskedPlan p = plan_masked(a);
+  if (a.n_rows <= 0) return 0;
+  const MaskedPlan p = plan_masked(a, is_bf16);
   if (p.split.n_chunks <= 1) return 0;
-  return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (PROW + 2);
+  return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (a.g.head_dim + 4 + 2);
 }
 
 template <int KIND, bool GROUPED>
@@ -790,14 +938,13 @@ static hipError_t launch_tiles(const MaskedAttnArgs& a, const MaskedPlan& p, uns
   static std::atomic<unsigned long long> told{0};
   const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<KIND, GROUPED>, kTileBytes, told);
   if (e != hipSuccess) return e;
-  masked_attn_tile_kernel<KIND, GROUPED><<<grid, 256, kTileBytes, st>>>(a, p.split, p.slots, p.rows_per_tile, part_o, part_ml);
+  masked_attn_tile_kernel<KIND, GROUPED><<<grid, 256, kTileBytes, st>>>(a, p.split, (int)p.slots, p.rows_per_tile, part_o, part_ml);
   return hipGetLastError();
 }
 
 template <int KIND>
 static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, float* part_o, float2* part_ml, hipStream_t st) {
-  const long grid = (long)p.slots * p.split.n_chunks * a.g.n_kv_heads;
-  if (grid > INT_MAX) return hipErrorInvalidValue;
+  const long grid = p.slots * p.split.n_chunks * a.g.n_kv_heads;
   if (p.rows) {
     static std::atomic<unsigned long long> told{0};
     const hipError_t e = allow_dynamic_lds((const void*)masked_attn_rows_kernel<KIND>, 4 * kRowWaveBytes, told);
@@ -813,28 +960,28 @@ static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, floa
 }
 
 hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float* part, hipStream_t st) {
-  const unsigned per_row = (unsigned)(((long)a.n_rows * a.n_q_heads + 3) / 4);
-  if (!is_bf16) {
-    masked_attn_f32_kernel<<<per_row, 256, 0, st>>>(a);
-    return hipGetLastError();
-  }
-  MaskedPlan p = plan_masked(a);
+  MaskedPlan p = plan_masked(a, is_bf16);
   if (!part) p.split = {1, 0};
-  float2* const part_ml = reinterpret_cast<float2*>(part + (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * PROW);
+  const long grid = p.slots * p.split.n_chunks * a.g.n_kv_heads, per_row = ((long)a.n_rows * a.n_q_heads + 3) / 4;
+  if (grid > INT_MAX || per_row > INT_MAX) return hipErrorInvalidValue;
+  float2* const part_ml = reinterpret_cast<float2*>(part + (size_t)grid * p.cols * (a.g.head_dim + 4));
   const bool cap = a.cap > 0.f, bias = a.slopes != nullptr;
   hipError_t e;
-  if (cap && bias) e = launch_bf16<kCapBias>(a, p, part, part_ml, st);
+  if (!is_bf16) {
+    if (a.g.head_dim == 64) masked_attn_f32_kernel<64><<<(unsigned)grid, 512, 0, st>>>(a, p.split, (int)p.slots, part, part_ml);
+    else masked_attn_f32_kernel<128><<<(unsigned)grid, 256, 0, st>>>(a, p.split, (int)p.slots, part, part_ml);
+    e = hipGetLastError();
+  } else if (cap && bias) e = launch_bf16<kCapBias>(a, p, part, part_ml, st);
   else if (bias) e = launch_bf16<kBias>(a, p, part, part_ml, st);
   else if (!cap) e = launch_bf16<kPlain>(a, p, part, part_ml, st);
   else if (a.cap * kLog2e <= kMostBounded) e = launch_bf16<kBounded>(a, p, part, part_ml, st);
   else e = launch_bf16<kCap>(a, p, part, part_ml, st);
   if (e != hipSuccess || p.split.n_chunks <= 1) return e;
-  if (p.rows) {
-    const unsigned grid = (unsigned)(((long)a.n_seq * a.max_rows_per_seq * a.n_q_heads + 3) / 4);
-    masked_attn_merge_kernel<true><<<grid, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
-  } else {
-    masked_attn_merge_kernel<false><<<per_row, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
-  }
+  const unsigned rows = (unsigned)per_row, by_seq = (unsigned)(((long)a.n_seq * a.max_rows_per_seq * a.n_q_heads + 3) / 4);
+  if (p.rows) masked_attn_merge_kernel<bf16, DH, ROW_COLS, true><<<by_seq, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
+  else if (is_bf16) masked_attn_merge_kernel<bf16, DH, TILE_COLS, false><<<rows, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
+  else if (a.g.head_dim == 64) masked_attn_merge_kernel<float, 64, F32_COLS, false><<<rows, 256, 0, st>>>(a, p.split, 0, part, part_ml);
+  else masked_attn_merge_kernel<float, 128, F32_COLS, false><<<rows, 256, 0, st>>>(a, p.split, 0, part, part_ml);
   return hipGetLastError();
 }
 
