@@ -244,7 +244,8 @@ def _stream(stream) -> Optional[int]:
     if stream is None:
         if not torch.cuda.is_available():
             return None          # host-side argument checks need no stream
-        stream = torch.cuda.current_stream()
+        # the current stream of the current device, without the object that torch.cuda.current_stream() makes (2.6 us a call)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
     return stream.cuda_stream or None
 
 
@@ -632,12 +633,14 @@ def rc_rotary_init(layout: int, rotary_dim: int, base: float, scaling: int = RC_
 
 
 def _i32(t: Optional[torch.Tensor], n: int, what: str) -> Optional[int]:
-    if t is not None and (t.dtype != torch.int32 or t.numel() < n):
-        raise ValueError(f"{what}: {n} int32 values expected, got {t.numel()} of {t.dtype}")
-    return _ptr(t)
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{what}: {n} contiguous int32 values expected, got {t.numel()} of {t.dtype}")
+    return t.data_ptr()
 
 
-@dataclass
+@dataclass(frozen=True)
 class BatchRows:
     """What rc_batch_map writes: int32 device tensors, of one element per row (but row_start, kv_len, counts)."""
     row_start: torch.Tensor                    # [n_seq + 1]
@@ -649,6 +652,16 @@ class BatchRows:
     kv_len: Optional[torch.Tensor]             # [n_seq]
     counts: Optional[torch.Tensor]             # [3]: rows, next free entry, refused sequences
 
+    def __post_init__(self):
+        per_row = (self.row_seq, self.row_pos, self.row_slot, self.row_lo, self.row_hi)
+        sizes = [int(t.numel()) for t in per_row if t is not None]
+        if not sizes:
+            raise ValueError("BatchRows: at least one array of the rows")
+        n_seq = int(self.row_start.numel()) - 1
+        out = [_i32(self.row_start, 1, "row_start"), *[_i32(t, 0, "rows") for t in per_row],
+               _i32(self.kv_len, n_seq, "kv_len"), _i32(self.counts, 3, "counts")]
+        object.__setattr__(self, "c", (n_seq, min(sizes), out))
+
     @staticmethod
     def alloc(n_seq: int, max_rows: int, device="cuda") -> "BatchRows":
         z = lambda n: torch.zeros(n, dtype=torch.int32, device=device)
@@ -659,19 +672,15 @@ def rc_batch_map(n_cached: torch.Tensor, n_new: torch.Tensor, block_table: torch
                  free_blocks: torch.Tensor, rows: BatchRows, free_first: Optional[torch.Tensor] = None,
                  prefix_len: Optional[torch.Tensor] = None, doc_start: Optional[torch.Tensor] = None,
                  doc_first: Optional[torch.Tensor] = None, stream=None) -> None:
-    n_seq = int(n_new.numel())
-    per_row = [t for t in (rows.row_seq, rows.row_pos, rows.row_slot, rows.row_lo, rows.row_hi) if t is not None]
-    max_rows = min((int(t.numel()) for t in per_row), default=2 ** 31 - 1)
-    if block_table.dim() != 2 or block_table.shape[0] < n_seq or block_table.dtype != torch.int32:
-        raise ValueError(f"block_table: int32 [{n_seq}][blocks] expected")
-    a = rc_batch_map_args(n_seq, max_rows, _i32(n_cached, n_seq, "n_cached"), _ptr(n_new), _ptr(block_table), block_table.shape[1],
-                          block_size, n_blocks, free_blocks.numel(), _i32(free_blocks, 0, "free_blocks") or None,
-                          _i32(free_first, 1, "free_first"), _i32(prefix_len, n_seq, "prefix_len"),
-                          _i32(doc_start, n_seq + 1, "doc_start"), _i32(doc_first, 0, "doc_first"),
-                          0 if doc_first is None else doc_first.numel(), _i32(rows.row_start, n_seq + 1, "row_start"),
-                          _i32(rows.row_seq, 0, "row_seq"), _i32(rows.row_pos, 0, "row_pos"), _i32(rows.row_slot, 0, "row_slot"),
-                          _i32(rows.row_lo, 0, "row_lo"), _i32(rows.row_hi, 0, "row_hi"), _i32(rows.kv_len, n_seq, "kv_len"),
-                          _i32(rows.counts, 3, "counts"))
+    """The sequences are those of rows.row_start; the block table has a row for each."""
+    n_seq, max_rows, out = rows.c
+    if n_new.numel() != n_seq or block_table.dim() != 2 or block_table.shape[0] < n_seq:
+        raise ValueError(f"n_new [{n_seq}] and block_table [{n_seq}][blocks] expected")
+    a = rc_batch_map_args(n_seq, max_rows, _i32(n_cached, n_seq, "n_cached"), _i32(n_new, n_seq, "n_new"),
+                          _i32(block_table, 0, "block_table"), block_table.shape[1], block_size, n_blocks, free_blocks.numel(),
+                          _i32(free_blocks, 0, "free_blocks") or None, _i32(free_first, 1, "free_first"),
+                          _i32(prefix_len, n_seq, "prefix_len"), _i32(doc_start, n_seq + 1, "doc_start"),
+                          _i32(doc_first, 0, "doc_first"), 0 if doc_first is None else doc_first.numel(), *out)
     _check(lib.rc_batch_map(C.byref(a), _stream(stream)), "rc_batch_map")
 
 
@@ -695,7 +704,7 @@ def rc_rotary_move(src: rc_kv_layer, src_slot: torch.Tensor, dst: rc_kv_layer, d
                               _i32(old_pos, n, "old_pos"), _stream(stream)), "rc_rotary_move")
 
 
-@dataclass
+@dataclass(frozen=True)
 class MaskedAttention:
     """The rows of a ragged batch as rc_masked_attention takes them (int32 device tensors, slopes float32)."""
     row_start: torch.Tensor                    # [n_seq + 1]
@@ -710,22 +719,26 @@ class MaskedAttention:
     scale: float = 0.0                         # 0: 1 / sqrt(head_dim)
     cap: float = 0.0                           # 0: none
 
-    def c(self) -> rc_masked_attention_args:
-        n_seq = int(self.row_start.numel()) - 1
-        return rc_masked_attention_args(n_seq, self.n_rows, self.max_rows_per_seq, self.max_len, _i32(self.row_start, 1, "row_start"),
-                                        _i32(self.row_pos, self.n_rows, "row_pos"), _i32(self.row_lo, self.n_rows, "row_lo"),
-                                        _i32(self.row_hi, self.n_rows, "row_hi"), _i32(self.seq, n_seq, "seq"), _ptr(self.slopes),
-                                        self.scale, self.cap)
+    def __post_init__(self):
+        n_seq, n = int(self.row_start.numel()) - 1, max(self.n_rows, 0)
+        if self.slopes is not None and self.slopes.dtype is not torch.float32:
+            raise ValueError("slopes: float32 expected")
+        object.__setattr__(self, "c", rc_masked_attention_args(
+            n_seq, self.n_rows, self.max_rows_per_seq, self.max_len, _i32(self.row_start, 1, "row_start"),
+            _i32(self.row_pos, n, "row_pos"), _i32(self.row_lo, n, "row_lo"), _i32(self.row_hi, n, "row_hi"),
+            _i32(self.seq, n_seq, "seq"), _ptr(self.slopes), self.scale, self.cap))
 
 
 def rc_masked_attention_workspace_bytes(rows: MaskedAttention, n_q_heads: int, cache: rc_kv_layer) -> int:
-    return int(lib.rc_masked_attention_workspace_bytes(C.byref(rows.c()), n_q_heads, C.byref(cache)))
+    return int(lib.rc_masked_attention_workspace_bytes(C.byref(rows.c), n_q_heads, C.byref(cache)))
 
 
 def rc_masked_attention(q: torch.Tensor, rows: MaskedAttention, n_q_heads: int, cache: rc_kv_layer, out: torch.Tensor,
                         workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    if rows.slopes is not None and rows.slopes.numel() < n_q_heads:
+        raise ValueError(f"slopes: {n_q_heads} expected")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.rc_masked_attention(_ptr(q), C.byref(rows.c()), n_q_heads, C.byref(cache), _ptr(out), _ptr(workspace), nbytes,
+    _check(lib.rc_masked_attention(_ptr(q), C.byref(rows.c), n_q_heads, C.byref(cache), _ptr(out), _ptr(workspace), nbytes,
                                    _stream(stream)), "rc_masked_attention")
 
 
