@@ -166,174 +166,209 @@ __device__ inline float2 rotary_entry(double pos, double turns, float amplitude)
   return quarter & 2 ? make_float2(-amplitude * x, -amplitude * y) : make_float2(amplitude * x, amplitude * y);
 }
 
-// Eight elements of a head belong to a lane t of head_dim / 8: two runs of four, the elements of four rotary pairs (4t .. 4t + 3) where
-// 8t < rotary_dim, else eight that pass through.
-struct HeadLane { int off0, off1; bool rotated; };
-__device__ inline HeadLane head_lane(int t, int layout, int rotary_dim) {
-  HeadLane h;
-  h.rotated = 8 * t < rotary_dim;
+// 2 CH elements of a head belong to a lane t of head_dim / (2 CH): two runs of CH, the elements of CH rotary pairs (CH t .. CH t + CH - 1) where
+// 2 CH t < rotary_dim, else as many that pass through.  A run is 16 bytes of T: CH is 4 for float and 8 for bf16, 4 there where the
+// rotated part is no multiple of 16.
+template <int CH> struct HeadLane { int off0, off1; bool rotated; };
+template <int CH>
+__device__ inline HeadLane<CH> head_lane(int t, int layout, int rotary_dim) {
+  HeadLane<CH> h;
+  h.rotated = 2 * CH * t < rotary_dim;
   const bool apart = h.rotated && layout == RC_ROTARY_HALF;
-  h.off0 = apart ? 4 * t : 8 * t;
-  h.off1 = apart ? rotary_dim / 2 + 4 * t : 8 * t + 4;
+  h.off0 = apart ? CH * t : 2 * CH * t;
+  h.off1 = apart ? rotary_dim / 2 + CH * t : 2 * CH * t + CH;
   return h;
 }
-__device__ inline void rotate_pairs(float (&x0)[4], float (&x1)[4], const float2 (&cs)[4], int layout) {
+// cs: (cos, sin) of the lane's pairs
+template <int CH>
+__device__ inline void rotate_pairs(float (&x0)[CH], float (&x1)[CH], const float2* cs, int layout) {
   if (layout == RC_ROTARY_HALF) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < CH; ++e) {
+      const float2 t = cs[e];
       const float a = x0[e], b = x1[e];
-      x0[e] = a * cs[e].x - b * cs[e].y;
-      x1[e] = b * cs[e].x + a * cs[e].y;
+      x0[e] = a * t.x - b * t.y;
+      x1[e] = b * t.x + a * t.y;
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 4; e += 2) {
+    for (int e = 0; e < CH; e += 2) {
+      const float2 t = cs[e / 2], u = cs[CH / 2 + e / 2];
       const float a = x0[e], b = x0[e + 1], c = x1[e], d = x1[e + 1];
-      x0[e] = a * cs[e / 2].x - b * cs[e / 2].y;
-      x0[e + 1] = b * cs[e / 2].x + a * cs[e / 2].y;
-      x1[e] = c * cs[2 + e / 2].x - d * cs[2 + e / 2].y;
-      x1[e + 1] = d * cs[2 + e / 2].x + c * cs[2 + e / 2].y;
+      x0[e] = a * t.x - b * t.y;
+      x0[e + 1] = b * t.x + a * t.y;
+      x1[e] = c * u.x - d * u.y;
+      x1[e + 1] = d * u.x + c * u.y;
     }
   }
 }
 
-// four consecutive elements
-__device__ inline void load4(const float* p, float (&v)[4]) {
-  const float4 t = *reinterpret_cast<const float4*>(p);
-  v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+// CH consecutive elements
+template <int CH>
+__device__ inline void load_run(const float* p, float (&v)[CH]) {
+#pragma unroll
+  for (int i = 0; i < CH; i += 4) {
+    const float4 t = *reinterpret_cast<const float4*>(p + i);
+    v[i] = t.x; v[i + 1] = t.y; v[i + 2] = t.z; v[i + 3] = t.w;
+  }
 }
-__device__ inline void load4(const bf16* p, float (&v)[4]) {
+__device__ inline void load_run(const bf16* p, float (&v)[8]) { Vec16<bf16>::load(p, v); }
+__device__ inline void load_run(const bf16* p, float (&v)[4]) {
   const uint2 t = *reinterpret_cast<const uint2*>(p);
   v[0] = __uint_as_float(t.x << 16); v[1] = __uint_as_float(t.x & 0xffff0000u);
   v[2] = __uint_as_float(t.y << 16); v[3] = __uint_as_float(t.y & 0xffff0000u);
 }
-__device__ inline void store4(float* p, const float (&v)[4]) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
-__device__ inline void store4(bf16* p, const float (&v)[4]) {
+template <int CH>
+__device__ inline void store_run(float* p, const float (&v)[CH]) {
+#pragma unroll
+  for (int i = 0; i < CH; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+}
+__device__ inline void store_run(bf16* p, const float (&v)[8]) { Vec16<bf16>::store(p, v); }
+__device__ inline void store_run(bf16* p, const float (&v)[4]) {
   *reinterpret_cast<uint2*>(p) = make_uint2((uint32_t)f32_to_bf16(v[0]).v | ((uint32_t)f32_to_bf16(v[1]).v << 16),
                                             (uint32_t)f32_to_bf16(v[2]).v | ((uint32_t)f32_to_bf16(v[3]).v << 16));
 }
 
 // ------------------------------------------------------------------ per-head norm, rotation, scatter
-// A workgroup per row: its (cos, sin) once for all heads, then head_dim / 8 lanes a head.
-template <typename TI, typename T>
+// A workgroup per row: its (cos, sin) once for all heads, then head_dim / (2 CH) lanes a head; the loads of kHeadsAhead heads a lane stand in front of
+// the work on the first one.  Bound by HBM.
+static constexpr int kHeadsAhead = 2;
+template <typename TI, typename T, int CH>
 __global__ void __launch_bounds__(kThreads)
 norm_rotary_kernel(NormRotaryArgs a, RotaryArg rot) {
   __shared__ float2 cs_of[RC_ROTARY_MAX_PAIRS];
   const int r = blockIdx.x;
   if (a.n_live && r >= *a.n_live) return;
-  const int dh = a.g.head_dim, lph = dh / 8, per_pass = kThreads / lph;
+  const int dh = a.g.head_dim, lph = dh / (2 * CH), per_pass = kThreads / lph;
   const int t = threadIdx.x % lph, h0 = threadIdx.x / lph;
+  const HeadLane<CH> at = head_lane<CH>(t, rot.layout, rot.rotary_dim);
+  const int nq = a.n_q_heads, nkv = a.g.n_kv_heads, heads = nq + 2 * nkv;
+  const TI* const row = reinterpret_cast<const TI*>(a.qkv) + (size_t)r * a.stride;
+  float x0[kHeadsAhead][CH], x1[kHeadsAhead][CH];
+  auto load = [&](int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kHeadsAhead; ++u) {
+      const TI* const p = row + (size_t)min(h + u * per_pass, heads - 1) * dh;
+      load_run(p + at.off0, x0[u]);
+      load_run(p + at.off1, x1[u]);
+    }
+  };
+  load(h0);
   const int slot = a.slot[r];
   const bool to_cache = slot >= 0 && slot < a.g.rows;
   if ((int)threadIdx.x < rot.rotary_dim / 2)
     cs_of[threadIdx.x] = rotary_entry((double)a.pos[r], rot.turns[threadIdx.x], rot.amplitude);
   __syncthreads();
-  const HeadLane at = head_lane(t, rot.layout, rot.rotary_dim);
-  float2 cs[4];
+  for (int h1 = h0; h1 < heads; h1 += kHeadsAhead * per_pass) {
+    if (h1 != h0) load(h1);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) cs[e] = at.rotated ? cs_of[4 * t + e] : make_float2(1.f, 0.f);
-  const int nq = a.n_q_heads, nkv = a.g.n_kv_heads;
-  const TI* const row = reinterpret_cast<const TI*>(a.qkv) + (size_t)r * a.stride;
-  for (int h = h0; h < nq + 2 * nkv; h += per_pass) {
-    float x0[4], x1[4];
-    load4(row + (size_t)h * dh + at.off0, x0);
-    load4(row + (size_t)h * dh + at.off1, x1);
-    if (h >= nq + nkv) {
-      if (to_cache) {
-        T* const o = reinterpret_cast<T*>(a.v_pool) + slot_offset(a.g, slot, h - nq - nkv);
-        store4(o + at.off0, x0);
-        store4(o + at.off1, x1);
+    for (int u = 0; u < kHeadsAhead; ++u) {
+      const int h = h1 + u * per_pass;
+      if (h >= heads) break;
+      auto put = [&](T* p) __attribute__((always_inline)) {
+        store_run(p + at.off0, x0[u]);
+        store_run(p + at.off1, x1[u]);
+      };
+      if (h >= nq + nkv) {
+        if (to_cache) put(reinterpret_cast<T*>(a.v_pool) + slot_offset(a.g, slot, h - nq - nkv));
+        continue;
       }
-      continue;
-    }
-    const T* const gain = reinterpret_cast<const T*>(h < nq ? a.g_q : a.g_k);
-    if (gain) {
-      float ss = add_squares(add_squares(0.f, make_float4(x0[0], x0[1], x0[2], x0[3])), make_float4(x1[0], x1[1], x1[2], x1[3]));
-      for (int o = lph >> 1; o > 0; o >>= 1) ss += __shfl_xor(ss, o, 64);
-      const float inv = 1.0f / sqrtf(ss / (float)dh + a.eps);
-      float g0[4], g1[4];
-      load4(gain + at.off0, g0);
-      load4(gain + at.off1, g1);
+      const T* const gain = reinterpret_cast<const T*>(h < nq ? a.g_q : a.g_k);
+      if (gain) {
+        float ss = 0.f, g0[CH], g1[CH];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { x0[e] = x0[e] * inv * g0[e]; x1[e] = x1[e] * inv * g1[e]; }
-    }
-    if (h >= nq && to_cache && a.k_pre) {
-      T* const o = reinterpret_cast<T*>(a.k_pre) + slot_offset(a.g, slot, h - nq);
-      store4(o + at.off0, x0);
-      store4(o + at.off1, x1);
-    }
-    if (at.rotated) rotate_pairs(x0, x1, cs, rot.layout);
-    if (h < nq) {
-      T* const o = reinterpret_cast<T*>(a.q_out) + ((size_t)r * nq + h) * dh;
-      store4(o + at.off0, x0);
-      store4(o + at.off1, x1);
-    } else if (to_cache) {
-      T* const o = reinterpret_cast<T*>(a.k_pool) + slot_offset(a.g, slot, h - nq);
-      store4(o + at.off0, x0);
-      store4(o + at.off1, x1);
+        for (int e = 0; e < CH; e += 4) ss = add_squares(ss, make_float4(x0[u][e], x0[u][e + 1], x0[u][e + 2], x0[u][e + 3]));
+#pragma unroll
+        for (int e = 0; e < CH; e += 4) ss = add_squares(ss, make_float4(x1[u][e], x1[u][e + 1], x1[u][e + 2], x1[u][e + 3]));
+        for (int o = lph >> 1; o > 0; o >>= 1) ss += __shfl_xor(ss, o, 64);
+        const float inv = 1.0f / sqrtf(ss / (float)dh + a.eps);
+        load_run(gain + at.off0, g0);
+        load_run(gain + at.off1, g1);
+#pragma unroll
+        for (int e = 0; e < CH; ++e) { x0[u][e] = x0[u][e] * inv * g0[e]; x1[u][e] = x1[u][e] * inv * g1[e]; }
+      }
+      if (h >= nq && to_cache && a.k_pre) put(reinterpret_cast<T*>(a.k_pre) + slot_offset(a.g, slot, h - nq));
+      if (at.rotated) rotate_pairs(x0[u], x1[u], cs_of + CH * t, rot.layout);
+      if (h < nq) put(reinterpret_cast<T*>(a.q_out) + ((size_t)r * nq + h) * dh);
+      else if (to_cache) put(reinterpret_cast<T*>(a.k_pool) + slot_offset(a.g, slot, h - nq));
     }
   }
 }
 
 hipError_t launch_norm_rotary(const NormRotaryArgs& a, const RotaryArg& rot, bool qkv_bf16, bool pool_bf16, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  if (pool_bf16) {
-    if (qkv_bf16) norm_rotary_kernel<bf16, bf16><<<a.n, kThreads, 0, st>>>(a, rot);
-    else norm_rotary_kernel<float, bf16><<<a.n, kThreads, 0, st>>>(a, rot);
+  const bool wide = rot.rotary_dim % 16 == 0;
+  if (pool_bf16 && wide) {
+    if (qkv_bf16) norm_rotary_kernel<bf16, bf16, 8><<<a.n, kThreads, 0, st>>>(a, rot);
+    else norm_rotary_kernel<float, bf16, 8><<<a.n, kThreads, 0, st>>>(a, rot);
+  } else if (pool_bf16) {
+    if (qkv_bf16) norm_rotary_kernel<bf16, bf16, 4><<<a.n, kThreads, 0, st>>>(a, rot);
+    else norm_rotary_kernel<float, bf16, 4><<<a.n, kThreads, 0, st>>>(a, rot);
   } else {
-    if (qkv_bf16) norm_rotary_kernel<bf16, float><<<a.n, kThreads, 0, st>>>(a, rot);
-    else norm_rotary_kernel<float, float><<<a.n, kThreads, 0, st>>>(a, rot);
+    if (qkv_bf16) norm_rotary_kernel<bf16, float, 4><<<a.n, kThreads, 0, st>>>(a, rot);
+    else norm_rotary_kernel<float, float, 4><<<a.n, kThreads, 0, st>>>(a, rot);
   }
   return hipGetLastError();
 }
 
 // ------------------------------------------------------------------ rows to other slots and positions
-// head_dim / 8 lanes a (row, head): a lane reads and writes its pairs of the key and its eight elements of the value, so that a row may
-// stay in its slot.
-template <typename T>
+// head_dim / (2 CH) lanes a (row, head): a lane reads and writes its pairs of the key and its elements of the value, so that a row may stay in its
+// slot.  The (cos, sin) of a workgroup's rows are worked out once, under the loads.  Bound by HBM.
+template <typename T, int CH>
 __global__ void __launch_bounds__(kThreads)
 rotary_move_kernel(RotaryMoveArgs a, RotaryArg rot) {
-  const int dh = a.gs.head_dim, lph = dh / 8;
-  const long idx = (long)blockIdx.x * kThreads + threadIdx.x;
-  const int t = (int)(idx % lph);
-  const long rh = idx / lph;
-  const int head = (int)(rh % a.gs.n_kv_heads);
-  const long r = rh / a.gs.n_kv_heads;
-  if (r >= a.n || (a.n_live && r >= *a.n_live)) return;
-  const int from = a.src_slot[r], to = a.dst_slot[r];
-  if (from < 0 || from >= a.gs.rows || to < 0 || to >= a.gd.rows) return;
-  const size_t so = slot_offset(a.gs, from, head), dof = slot_offset(a.gd, to, head);
-  const HeadLane at = head_lane(t, rot.layout, rot.rotary_dim);
+  extern __shared__ float2 cs_rows[];   // [row of the workgroup][pair]
+  const int dh = a.gs.head_dim, lph = dh / (2 * CH), groups = kThreads / lph, nkv = a.gs.n_kv_heads, pairs = rot.rotary_dim / 2;
+  const long g0 = (long)blockIdx.x * groups;
+  const int r0 = (int)(g0 / nkv);
+  const int n = a.n_live ? min(a.n, *a.n_live) : a.n;
+  if (r0 >= n) return;
+  const int t = threadIdx.x % lph;
+  const long rh = g0 + threadIdx.x / lph;
+  const int r = (int)(rh / nkv), head = (int)(rh - (long)r * nkv);
+  const int rr = min(r, n - 1);
+  const int from = a.src_slot[rr], to = a.dst_slot[rr];
+  const bool moves = r < n && from >= 0 && from < a.gs.rows && to >= 0 && to < a.gd.rows;
+  const HeadLane<CH> at = head_lane<CH>(t, rot.layout, rot.rotary_dim);
+  const size_t so = slot_offset(a.gs, moves ? from : 0, head);
   const T* const k = reinterpret_cast<const T*>(a.k_src) + so;
   const T* const v = reinterpret_cast<const T*>(a.v_src) + so;
-  float x0[4], x1[4], v0[4], v1[4];
-  load4(k + at.off0, x0);
-  load4(k + at.off1, x1);
-  load4(v + at.off0, v0);
-  load4(v + at.off1, v1);
-  if (at.rotated) {
-    const double by = (double)a.new_pos[r] - (a.old_pos ? (double)a.old_pos[r] : 0.0);
-    const float amplitude = a.old_pos ? 1.f : rot.amplitude;
-    float2 cs[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) cs[e] = rotary_entry(by, rot.turns[4 * t + e], amplitude);
-    rotate_pairs(x0, x1, cs, rot.layout);
+  float x0[CH], x1[CH], v0[CH], v1[CH];
+  load_run(k + at.off0, x0);
+  load_run(k + at.off1, x1);
+  load_run(v + at.off0, v0);
+  load_run(v + at.off1, v1);
+  const int rows = (int)((g0 + groups - 1) / nkv) - r0 + 1;
+  for (int i = threadIdx.x; i < rows * pairs; i += kThreads) {
+    const int row = i / pairs, p = i - row * pairs, at_row = min(r0 + row, n - 1);
+    const double by = (double)a.new_pos[at_row] - (a.old_pos ? (double)a.old_pos[at_row] : 0.0);
+    cs_rows[i] = rotary_entry(by, rot.turns[p], a.old_pos ? 1.f : rot.amplitude);
   }
+  __syncthreads();
+  if (!moves) return;
+  if (at.rotated) rotate_pairs(x0, x1, cs_rows + (size_t)(r - r0) * pairs + CH * t, rot.layout);
+  const size_t dof = slot_offset(a.gd, to, head);
   T* const ko = reinterpret_cast<T*>(a.k_dst) + dof;
   T* const vo = reinterpret_cast<T*>(a.v_dst) + dof;
-  store4(ko + at.off0, x0);
-  store4(ko + at.off1, x1);
-  store4(vo + at.off0, v0);
-  store4(vo + at.off1, v1);
+  store_run(ko + at.off0, x0);
+  store_run(ko + at.off1, x1);
+  store_run(vo + at.off0, v0);
+  store_run(vo + at.off1, v1);
+}
+
+template <typename T, int CH>
+static hipError_t launch_move(const RotaryMoveArgs& a, const RotaryArg& rot, hipStream_t st) {
+  const int groups = kThreads / (a.gs.head_dim / (2 * CH)), nkv = a.gs.n_kv_heads;
+  const unsigned grid = (unsigned)(((long)a.n * nkv + groups - 1) / groups);
+  const int rows = (groups - 1) / nkv + 2;   // that the groups of a workgroup can touch
+  rotary_move_kernel<T, CH><<<grid, kThreads, (size_t)rows * (rot.rotary_dim / 2) * sizeof(float2), st>>>(a, rot);
+  return hipGetLastError();
 }
 
 hipError_t launch_rotary_move(const RotaryMoveArgs& a, const RotaryArg& rot, bool pool_bf16, hipStream_t st) {
   if (a.n <= 0) return hipSuccess;
-  const long work = (long)a.n * a.gs.n_kv_heads * (a.gs.head_dim / 8);
-  const unsigned grid = (unsigned)((work + kThreads - 1) / kThreads);
-  if (pool_bf16) rotary_move_kernel<bf16><<<grid, kThreads, 0, st>>>(a, rot);
-  else rotary_move_kernel<float><<<grid, kThreads, 0, st>>>(a, rot);
-  return hipGetLastError();
+  if (!pool_bf16) return launch_move<float, 4>(a, rot, st);
+  return rot.rotary_dim % 16 == 0 ? launch_move<bf16, 8>(a, rot, st) : launch_move<bf16, 4>(a, rot, st);
 }
 
 }  // namespace rc
