@@ -218,6 +218,20 @@ __device__ inline void load_run(const bf16* p, float (&v)[4]) {
   v[0] = __uint_as_float(t.x << 16); v[1] = __uint_as_float(t.x & 0xffff0000u);
   v[2] = __uint_as_float(t.y << 16); v[3] = __uint_as_float(t.y & 0xffff0000u);
 }
+// the same, of what nobody reads again: not kept in the caches on the way (5120 rows of float projections 39.6 -> 37.5 us; for cache rows and for
+// stores it is no gain: 32768 moved rows 57 -> 59 us with such loads, 87 with such stores)
+template <typename T, int CH>
+__device__ inline void load_run_once(const T* p, float (&v)[CH]) {
+  typedef unsigned u32xn __attribute__((ext_vector_type(CH * sizeof(T) >= 16 ? 4 : 2)));
+  constexpr int PER = sizeof(u32xn) / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < CH; i += PER) {
+    const u32xn t = __builtin_nontemporal_load(reinterpret_cast<const u32xn*>(p + i));
+#pragma unroll
+    for (int e = 0; e < PER; ++e)
+      v[i + e] = sizeof(T) == 4 ? __uint_as_float(t[e * sizeof(T) / 4]) : __uint_as_float(e & 1 ? t[e / 2] & 0xffff0000u : t[e / 2] << 16);
+  }
+}
 template <int CH>
 __device__ inline void store_run(float* p, const float (&v)[CH]) {
 #pragma unroll
@@ -249,8 +263,8 @@ norm_rotary_kernel(NormRotaryArgs a, RotaryArg rot) {
 #pragma unroll
     for (int u = 0; u < kHeadsAhead; ++u) {
       const TI* const p = row + (size_t)min(h + u * per_pass, heads - 1) * dh;
-      load_run(p + at.off0, x0[u]);
-      load_run(p + at.off1, x1[u]);
+      load_run_once(p + at.off0, x0[u]);
+      load_run_once(p + at.off1, x1[u]);
     }
   };
   load(h0);
