@@ -1469,7 +1469,7 @@ static rc_status masked_attention_args(const rc_masked_attention_args* d, int32_
   if (n_q_heads / cache->n_kv_heads > 128 || !aligned16({cache->k, cache->v})) return RC_E_UNSUPPORTED;
   if (d->n_seq > 65536 || (!d->seq && d->n_seq > cache->n_seq)) return RC_E_CAPACITY;
   if ((long)d->max_len > (long)cache->max_blocks_per_seq * cache->block_size || d->max_len > (1 << 30)) return RC_E_CAPACITY;
-  if ((long)cache->n_blocks * cache->block_size * cache->n_kv_heads > INT_MAX) return RC_E_CAPACITY;
+  if ((long)cache->n_blocks * cache->block_size * cache->n_kv_heads > INT_MAX || (long)d->n_rows * n_q_heads > INT_MAX) return RC_E_CAPACITY;
   *a = {};
   a->k_pool = cache->k;
   a->v_pool = cache->v;

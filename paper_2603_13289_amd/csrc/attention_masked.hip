@@ -234,12 +234,15 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   const Range mine = range_of_row(a, row);
   const unsigned seen = mine.hi < 0 ? 0u : (unsigned)(mine.hi - mine.lo) + 1u;
 
-  bf16x8 qf[8];
-  {
-    const bf16* const q = reinterpret_cast<const bf16*>(a.q) + ((size_t)row * a.n_q_heads + head) * DH + 8 * half;
+  // Queries come in whole rows and are handed around through the memory of the first V tiles (a wavefront's own part of it): with a lane asking for pieces of
+  // its own row, a load touched 64 cache lines.
+  const unsigned row_head = (unsigned)row * (unsigned)a.n_q_heads + (unsigned)head;   // below 2^31 (host)
+  unsigned char* const own_rows = lds + 2 * K_TILE + wave * 32 * KROW;
+  static_assert(TILE_COLS * KROW <= 2 * V_TILE, "room for the queries");
+  auto row_at = [&](int i) __attribute__((always_inline)) { return (size_t)(unsigned)__shfl((int)row_head, 4 * i + (lane >> 4), 64) * 256 + (lane & 15) * 16; };
+  u32x4 q_in[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) qf[i] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q + 16 * i));
-  }
+  for (int i = 0; i < 8; ++i) q_in[i] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(a.q) + row_at(i));
   Score<KIND> score(a);
   constexpr bool CAP = Score<KIND>::CAP, BIAS = Score<KIND>::BIAS;
   if constexpr (BIAS) score.slope = a.slopes[head] * kLog2e;
@@ -305,12 +308,21 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   const std::integral_constant<int, 0> buf0;
   const std::integral_constant<int, 1> buf1;
   Asked asked = {};   // of the tile two on
+  bf16x8 qf[8];
+  auto hand_queries = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<u32x4*>(own_rows + (4 * i + (lane >> 4)) * KROW + (lane & 15) * 16) = q_in[i];
+    asm volatile("" ::: "memory");   // a wavefront's LDS accesses stay in order
+#pragma unroll
+    for (int i = 0; i < 8; ++i) qf[i] = k_fragment(own_rows + k_lane(lane), 0, i);
+  };
   if (tid == 0) bad_v = 0;
   if (t_begin < t_end) {
     const Asked q0 = ask(t_begin), q1 = ask(t_begin + 1);
     asked = ask(t_begin + 2);
     fetch(q0);
-    __syncthreads();
+    hand_queries();
+    __syncthreads();   // the queries are in registers: V may come where they were
     clean_v(t_begin);
     stage_k(buf0);
 #pragma unroll
@@ -440,8 +452,8 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   }
 
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-  if (!live) return;
   if (is_split) {
+    if (!live) return;
     const size_t at = ((size_t)(slot * (long)sp.n_chunks + chunk) * a.g.n_kv_heads + kvh) * TILE_COLS + col;
     if (half == 0) part_ml[at] = make_float2(m_run, l_tot);
     float* const o = part_o + at * PROW + 4 * half;
@@ -452,13 +464,21 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
         *reinterpret_cast<float4*>(o + 32 * db + 2 * e) = make_float4(acc_o[db][e], acc_o[db][e + 1], acc_o[db][e + 2], acc_o[db][e + 3]);
     return;
   }
+  // outputs leave as whole rows, the way the queries came
   const float inv = seen ? 1.0f / l_tot : 0.f;
-  bf16* const o = reinterpret_cast<bf16*>(a.out) + ((size_t)row * a.n_q_heads + head) * DH + 4 * half;
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
     for (int e = 0; e < 16; e += 4)
-      *reinterpret_cast<uint2*>(o + 32 * db + 2 * e) = pack4(acc_o[db][e] * inv, acc_o[db][e + 1] * inv, acc_o[db][e + 2] * inv, acc_o[db][e + 3] * inv);
+      *reinterpret_cast<uint2*>(own_rows + ql * KROW + 64 * db + 4 * e + 8 * half) = pack4(acc_o[db][e] * inv, acc_o[db][e + 1] * inv, acc_o[db][e + 2] * inv, acc_o[db][e + 3] * inv);
+  asm volatile("" ::: "memory");
+  const unsigned long long live_cols = __ballot(live);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const size_t to = row_at(i);
+    const u32x4 o = *reinterpret_cast<const u32x4*>(own_rows + (4 * i + (lane >> 4)) * KROW + (lane & 15) * 16);
+    if (live_cols >> (4 * i + (lane >> 4)) & 1) *reinterpret_cast<u32x4*>(reinterpret_cast<char*>(a.out) + to) = o;
+  }
 }
 
 // ------------------------------------------------------------------ few rows a sequence: at most 32 columns
