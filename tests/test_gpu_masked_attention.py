@@ -63,7 +63,8 @@ class Batch:
     def check(self, got, cap=0.0, bias=False, scale=0.0, rows=None):
         """Tolerance, from the arithmetic.  A score is a sum of dh products in 32 bits (at most dh + 2 roundings of its absolute sum), the capped
         score adds four roundings of the cap, the bias two of its own size; an error d of scores changes weights by 2d relative.
-        Weights are rounded to the type for the second product (bf16: half a step), sums of at most 4096 terms per accumulator in 32 bits, the output once to the type."""
+        Weights are rounded to the type for the second product (bf16: half a step) and added up as rounded, so each moves the quotient by half a step of
+        its share of |v - out|, at most of mass + |out|; sums of at most 4096 terms per accumulator in 32 bits, the output once to the type."""
         g = got.double().cpu().numpy()
         assert np.isfinite(g[:self.n]).all()
         slopes = self.slopes() if bias else None
@@ -82,7 +83,7 @@ class Batch:
                 d = d + 2 * u * (slopes.max() * reach)[:, None, None]
             half = ref.step_of(self.td)
             weights = half if self.code == rc.RC_BF16 else 0.0
-            bound = (weights + 2 * d + 4096 * u) * mass * (1 + 2 ** -7) + half * np.abs(want) * (1 + 2 ** -7) + 1e-30
+            bound = (weights + 2 * d + 4096 * u) * mass * (1 + 2 ** -7) + (half + weights) * np.abs(want) * (1 + 2 ** -7) + 1e-30
             err = np.abs(g[at] - want)
             assert (err <= bound).all(), (s, float((err - bound).max()), float(err.max()))
 
