@@ -461,15 +461,16 @@ typedef struct {
 /* Host function: fills *out, a plain host struct that the calls below read during the call only. */
 RC_API rc_status rc_rotary_init(const rc_rotary_desc* desc, rc_rotary* out);
 
-/* Block tables, slots and key ranges of a step.  Sequence s holds n_cached[s] rows and gets n_new[s] more (0 is fine, a
- * negative count is one).  Blocks that the new rows need are taken from free_blocks in the order of the sequences, starting at entry *free_first,
+/* Block tables, slots and key ranges of a step.  Sequence s holds n_cached[s] rows and gets n_new[s] more (0 is fine, and a
+ * negative count counts as 0).  Blocks that the new rows need are taken from free_blocks in the order of the sequences, starting at entry *free_first,
  * and entered in the block table; the entries of blocks that a sequence has already stay as they are.
  * A sequence is refused as a whole where its rows would not fit its block table, the free list or max_rows: it takes no block,
  * its rows get slot -1 and see no key (lo 0, hi -1), the other sequences are served.  (Behind the one that the free list is too short for,
  * only sequences that need no block are.)
  * Keys that a row may see, both ends included: row_lo = first position of its document, row_hi = min(max(position,
  * prefix_len - 1), last position of its document).
- * Outputs may not be inputs' memory (kv_len is not n_cached, counts does not hold free_first), but for block_table. */
+ * No output may overlap an input (kv_len is not n_cached, counts does not hold free_first): RC_E_INVALID_ARG.  Other errors: RC_E_CAPACITY (n_seq, pool
+ * or table rows of 2^31). */
 typedef struct {
   int32_t n_seq;               /* 1 .. 65536 */
   int32_t max_rows;            /* rows that the row arrays have room for, >= 0 */
@@ -497,7 +498,7 @@ RC_API rc_status rc_batch_map(const rc_batch_map_args* args, void* stream);
  * then rotated; queries go to q_out [n][Hq][dh] of T, keys and values into slot[i] of dst, keys before the rotation into slot[i] of the
  * pool k_pre (optional, dst's geometry).  Sums and rotations are of 32 bits (angles of 64), and a result is rounded once.
  * n_live (optional, device): rows that there are, where n is only a bound (rc_batch_map: row_start + n_seq).
- * All arrays 16-byte aligned.  Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (stride, alignment, head_dim), RC_E_CAPACITY (pool of 2^31 rows). */
+ * All arrays 16-byte aligned; q_out may not overlap qkv.  Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (stride, alignment, head_dim), RC_E_CAPACITY (pool of 2^31 rows). */
 RC_API rc_status rc_norm_rotary_rows(const void* qkv, int32_t qkv_dtype, int64_t qkv_stride, int32_t n, const int32_t* n_live,
                                      int32_t n_q_heads, const void* g_q, const void* g_k, float eps, const rc_rotary* rotary,
                                      const int32_t* pos, const int32_t* slot, const rc_kv_layer* dst, void* k_pre, void* q_out,
@@ -506,7 +507,8 @@ RC_API rc_status rc_norm_rotary_rows(const void* qkv, int32_t qkv_dtype, int64_t
 /* Rows of one layer's cache moved to other slots and positions, of any sequences at once: row i goes from src_slot[i] of src to
  * dst_slot[i] of dst, its key rotated from old_pos[i] to new_pos[i] (old_pos NULL: keys stored before rotation, rotated to new_pos[i] and
  * multiplied by the amplitude, which rotated keys have already), its value copied.  src and dst have equal n_kv_heads, head_dim, dtype and may be one cache if
- * every row of the call stays in its slot or no row's destination is another's source.  n_live as above. */
+ * every row of the call stays in its slot or no row's destination is another's source.  A row with a slot outside its pool is not moved.  n_live as
+ * above.  Errors: as rc_norm_rotary_rows; RC_E_CAPACITY also where n * n_kv_heads passes 2^31. */
 RC_API rc_status rc_rotary_move(const rc_kv_layer* src, const int32_t* src_slot, const rc_kv_layer* dst, const int32_t* dst_slot,
                                 int32_t n, const int32_t* n_live, const rc_rotary* rotary, const int32_t* new_pos,
                                 const int32_t* old_pos, void* stream);
@@ -517,8 +519,9 @@ RC_API rc_status rc_rotary_move(const rc_kv_layer* src, const int32_t* src_slot,
  * Key ranges are cut to [0, max_len).  Causal attention is row_lo NULL (0) and row_hi NULL (row_pos); sliding windows, documents and prefixes are ranges
  * (rc_batch_map).  Keys and values outside a row's range do not touch it, whatever they hold.  q, out: [n_rows][Hq][dh] of T.
  * workspace (optional, device, 256-byte aligned, rc_masked_attention_workspace_bytes): lets long key ranges be cut where the batch has few rows; NULL: not cut.
- * Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (more than 128 query heads on a key head, alignment), RC_E_CAPACITY (max_len beyond the block table, n_seq),
- * RC_E_WORKSPACE. */
+ * Calls that overlap in time need workspaces of their own.  A result does not depend on other sequences' rows but through how ranges are cut.
+ * Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (more than 128 query heads on a key head, alignment, bf16 with a cap above 4096), RC_E_CAPACITY (max_len
+ * beyond the block table or 2^30, n_seq, n_rows * n_q_heads or pool rows of 2^31), RC_E_WORKSPACE. */
 typedef struct {
   int32_t n_seq;               /* 1 .. 65536 */
   int32_t n_rows;              /* rows of q and out; row_start[n_seq] is at most that */

@@ -689,8 +689,14 @@ def rc_norm_rotary_rows(qkv: torch.Tensor, n: int, n_q_heads: int, rotary: rc_ro
                         g_k: Optional[torch.Tensor] = None, eps: float = 1e-5, k_pre: Optional[torch.Tensor] = None,
                         n_live: Optional[torch.Tensor] = None, stream=None) -> None:
     """qkv: [rows][width], float32 or bf16, rows any multiple of 4 elements apart."""
-    assert qkv.dim() == 2 and qkv.stride(1) == 1 and qkv.dtype in (torch.float32, torch.bfloat16)
-    dtype = RC_BF16 if qkv.dtype == torch.bfloat16 else RC_F32
+    td = torch_dtype(dst.dtype)
+    if qkv.dim() != 2 or qkv.stride(1) != 1 or qkv.shape[0] < n or qkv.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"qkv: float32 or bf16 [{n}][width] expected")
+    if q_out.dtype is not td or q_out.numel() < n * n_q_heads * dst.head_dim:
+        raise ValueError(f"q_out: {td} [{n}][{n_q_heads}][{dst.head_dim}] expected")
+    if any(g is not None and (g.dtype is not td or g.numel() != dst.head_dim) for g in (g_q, g_k)):
+        raise ValueError(f"gains: {td} [{dst.head_dim}] expected")
+    dtype = RC_BF16 if qkv.dtype is torch.bfloat16 else RC_F32
     _check(lib.rc_norm_rotary_rows(qkv.data_ptr(), dtype, qkv.stride(0), n, _i32(n_live, 1, "n_live"), n_q_heads, _ptr(g_q),
                                    _ptr(g_k), eps, C.byref(rotary), _i32(pos, n, "pos"), _i32(slot, n, "slot"), C.byref(dst),
                                    _ptr(k_pre), _ptr(q_out), _stream(stream)), "rc_norm_rotary_rows")
@@ -737,6 +743,9 @@ def rc_masked_attention(q: torch.Tensor, rows: MaskedAttention, n_q_heads: int, 
                         workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     if rows.slopes is not None and rows.slopes.numel() < n_q_heads:
         raise ValueError(f"slopes: {n_q_heads} expected")
+    need = max(rows.n_rows, 0) * n_q_heads * cache.head_dim
+    if out is not None and (q.numel() < need or out.numel() < need or q.dtype is not out.dtype or q.dtype is not torch_dtype(cache.dtype)):
+        raise ValueError(f"q, out: {torch_dtype(cache.dtype)} [{rows.n_rows}][{n_q_heads}][{cache.head_dim}] expected")
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib.rc_masked_attention(_ptr(q), C.byref(rows.c), n_q_heads, C.byref(cache), _ptr(out), _ptr(workspace), nbytes,
                                    _stream(stream)), "rc_masked_attention")

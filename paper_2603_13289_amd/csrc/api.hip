@@ -1419,9 +1419,15 @@ rc_status rc_batch_map(const rc_batch_map_args* a, void* stream) {
     return RC_E_INVALID_ARG;
   if (a->n_free > 0 && !a->free_blocks) return RC_E_INVALID_ARG;
   if (a->n_docs > 0 && (!a->doc_start || !a->doc_first)) return RC_E_INVALID_ARG;
-  // every workgroup reads the lengths, one of them writes these: they have to be apart
-  if (a->kv_len && (a->kv_len == a->n_cached || a->kv_len == a->n_new)) return RC_E_INVALID_ARG;
-  if (a->counts && a->free_first >= a->counts && a->free_first < a->counts + 3) return RC_E_INVALID_ARG;
+  // every workgroup reads the inputs while some write the outputs: they have to be apart
+  struct Span { const int32_t* p; long n; };
+  const long n = a->n_seq, rows = a->max_rows;
+  const Span in[] = {{a->n_cached, n}, {a->n_new, n}, {a->free_blocks, a->n_free}, {a->free_first, 1}, {a->prefix_len, n}, {a->doc_start, n + 1}, {a->doc_first, a->n_docs}};
+  const Span out[] = {{a->block_table, n * a->max_blocks_per_seq}, {a->row_start, n + 1}, {a->row_seq, rows}, {a->row_pos, rows}, {a->row_slot, rows},
+                      {a->row_lo, rows}, {a->row_hi, rows}, {a->kv_len, n}, {a->counts, 3}};
+  for (const Span& o : out)
+    for (const Span& i : in)
+      if (o.p && i.p && o.p < i.p + i.n && i.p < o.p + o.n) return RC_E_INVALID_ARG;
   if (a->n_seq > 65536 || (long)a->n_blocks * a->block_size > INT_MAX || (long)a->max_blocks_per_seq * a->block_size > INT_MAX)
     return RC_E_CAPACITY;
   RC_HIP(launch_batch_map(*a, reinterpret_cast<hipStream_t>(stream)));
@@ -1437,6 +1443,12 @@ rc_status rc_norm_rotary_rows(const void* qkv, int32_t qkv_dtype, int64_t qkv_st
   if (!qkv || !pos || !slot || !q_out || n < 0 || n_q_heads < 1 || n_q_heads % dst->n_kv_heads || !(eps >= 0.f)) return RC_E_INVALID_ARG;
   if (qkv_dtype != RC_F32 && qkv_dtype != RC_BF16) return RC_E_INVALID_ARG;
   if (qkv_stride < (int64_t)(n_q_heads + 2 * (int64_t)dst->n_kv_heads) * dst->head_dim) return RC_E_INVALID_ARG;
+  // a row's queries may not land where another row's projections wait to be read
+  const char* const in = reinterpret_cast<const char*>(qkv);
+  const char* const out = reinterpret_cast<const char*>(q_out);
+  const int64_t in_bytes = (int64_t)n * qkv_stride * (int64_t)elem_size(qkv_dtype), out_bytes = (int64_t)n * n_q_heads * dst->head_dim * (int64_t)elem_size(dst->dtype);
+  if (in < out + out_bytes && out < in + in_bytes) return RC_E_INVALID_ARG;
+  if (k_pre && (k_pre == dst->k || k_pre == dst->v)) return RC_E_INVALID_ARG;
   if (qkv_stride % 4 || !aligned16({qkv, g_q, g_k, k_pre, q_out})) return RC_E_UNSUPPORTED;
   NormRotaryArgs a = {qkv, (long)qkv_stride, n, n_q_heads, n_live, g_q, g_k, eps, pos, slot, {}, dst->k, dst->v, k_pre, q_out};
   RC_TRY(slot_geom_of(*dst, &a.g));
@@ -1456,6 +1468,7 @@ rc_status rc_rotary_move(const rc_kv_layer* src, const int32_t* src_slot, const 
   RotaryMoveArgs a = {src->k, src->v, dst->k, dst->v, {}, {}, src_slot, dst_slot, new_pos, old_pos, n_live, n};
   RC_TRY(slot_geom_of(*src, &a.gs));
   RC_TRY(slot_geom_of(*dst, &a.gd));
+  if ((long)n * src->n_kv_heads > INT_MAX) return RC_E_CAPACITY;
   if (n == 0) return RC_OK;
   RC_HIP(launch_rotary_move(a, rot, src->dtype == RC_BF16, reinterpret_cast<hipStream_t>(stream)));
   return RC_OK;
@@ -1467,6 +1480,7 @@ static rc_status masked_attention_args(const rc_masked_attention_args* d, int32_
   if (n_q_heads < 1 || n_q_heads % cache->n_kv_heads) return RC_E_INVALID_ARG;
   if (!(d->scale >= 0.f) || !(d->cap >= 0.f) || std::isinf(d->scale) || std::isinf(d->cap)) return RC_E_INVALID_ARG;
   if (n_q_heads / cache->n_kv_heads > 128 || !aligned16({cache->k, cache->v})) return RC_E_UNSUPPORTED;
+  if (cache->dtype == RC_BF16 && d->cap > kMostCap) return RC_E_UNSUPPORTED;
   if (d->n_seq > 65536 || (!d->seq && d->n_seq > cache->n_seq)) return RC_E_CAPACITY;
   if ((long)d->max_len > (long)cache->max_blocks_per_seq * cache->block_size || d->max_len > (1 << 30)) return RC_E_CAPACITY;
   if ((long)cache->n_blocks * cache->block_size * cache->n_kv_heads > INT_MAX || (long)d->n_rows * n_q_heads > INT_MAX) return RC_E_CAPACITY;

@@ -54,11 +54,12 @@ __device__ inline SeqRows rows_of_seq(const MaskedAttnArgs& a, int s, int start,
   return q;
 }
 __device__ inline SeqRows rows_of_seq(const MaskedAttnArgs& a, int s) { return rows_of_seq(a, s, a.row_start[s], a.row_start[s + 1]); }
-// Keys that a row sees; (INT_MAX, -1) where it sees none.
+// Keys that a row sees; (kNoKey, -1) where it sees none.
+static constexpr int kNoKey = 1 << 30;   // no key is that far (host)
 struct Range { int lo, hi; };
 __device__ inline Range range_of_row(const MaskedAttnArgs& a, int row) {
   const int lo = max(a.row_lo ? a.row_lo[row] : 0, 0), hi = min(a.row_hi ? a.row_hi[row] : a.row_pos[row], a.max_len - 1);
-  return lo <= hi ? Range{lo, hi} : Range{INT_MAX, -1};
+  return lo <= hi ? Range{lo, hi} : Range{kNoKey, -1};
 }
 // The last sequence s whose place(first row, s) is at most x; places ascend.  64 candidates a step, and the starts of the last 64 stay in the lanes.
 template <typename F>
@@ -78,8 +79,8 @@ __device__ inline SeqRows find_seq(const MaskedAttnArgs& a, int x, F place) {
 
 // Scores in units of log2 (what a weight is 2 to the power of), up to a line: score = raw * MUL + add, MUL and add the same for all keys, so
 // that the line and the reference exponent's subtraction are one operation.  The cap: cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1), whose
-// quotient is the raw score (it falls as the score rises); its error of 2^-23 changes a weight by as much times the cap, where weights are
-// rounded to 2^-9 in any case.
+// quotient is the raw score (it falls as the score rises); its error of 2^-23 changes a weight by as much times the cap (kMostCap: 2^-11), where weights
+// are rounded to 2^-9 in any case.
 // Bounded scores: a cap without a bias bounds them by itself, so that its softmax needs no running maximum: with the reference exponent fixed at half
 // the cap, weights lie between 2^-120 and 2^40 up to kMostBounded, and no score has to wait for another.
 enum ScoreKind : int { kPlain = 0, kBias = 1, kCap = 2, kCapBias = 3, kBounded = 4 };
@@ -90,7 +91,7 @@ struct Score {
   static constexpr bool kFalls = CAP && !BIAS;
   float in, out, mul, add, slope, from;   // from: key offset of the lane's element 0 minus the row's position
   __device__ Score(const MaskedAttnArgs& a)
-      : in(CAP ? 2.f * kLog2e * a.scale / a.cap : a.scale * kLog2e), out(-2.f * kLog2e * a.cap),
+      : in(CAP ? fminf(2.f * kLog2e * a.scale / a.cap, 3e38f) : a.scale * kLog2e), out(-2.f * kLog2e * a.cap),
         mul(BIAS ? 1.f : CAP ? out : in), add(CAP ? kLog2e * a.cap : 0.f), slope(0.f), from(0.f) {}
   __device__ __forceinline__ float raw(float dot, float offset) const {
     float x = dot;
@@ -155,8 +156,8 @@ __device__ __forceinline__ float move_reference(const Score<KIND>& score, const 
   }
   return score.add - (m_run == -INFINITY ? 0.f : m_run);
 }
-// The sum takes the weights as they are multiplied, rounded: where few keys count, their roundings then cancel in the quotient (two keys: error
-// 0.0017 -> 0.0011 against 64 bits, of which 0.0008 are the output's own rounding); and it takes two at a time.
+// The sum takes the weights as they are multiplied, rounded: where few keys count, their roundings then cancel in the quotient (tokens behind
+// a handful of keys: error against 64 bits 0.0017 -> 0.00085, of which 0.0008 are the output's own rounding); and it takes two at a time.
 __device__ __forceinline__ void add_weights(bf16x8 p, float& sum) {
   typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
   const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};

@@ -527,6 +527,7 @@ struct MaskedAttnArgs {
   const float* slopes;
   float scale, cap;
 };
+constexpr float kMostCap = 4096.f;   // of bf16: Score says why
 size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16);
 hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float* part, hipStream_t st);
 

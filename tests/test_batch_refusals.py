@@ -67,6 +67,9 @@ def test_batch_map_refusals():
     assert status(lambda: call(n_new=rows.kv_len)) == rc.RC_E_INVALID_ARG                       # an output that is an input
     assert status(lambda: call(n_cached=rows.kv_len)) == rc.RC_E_INVALID_ARG
     assert status(lambda: call(free_first=rows.counts[1:])) == rc.RC_E_INVALID_ARG
+    assert status(lambda: call(prefix_len=rows.row_start[1:])) == rc.RC_E_INVALID_ARG
+    assert status(lambda: call(n_cached=rows.row_hi[5:7])) == rc.RC_E_INVALID_ARG
+    assert status(lambda: call(n_cached=table.view(-1)[2:4])) == rc.RC_E_INVALID_ARG
     assert status(lambda: call(doc_first=ints(3))) == rc.RC_E_INVALID_ARG                       # documents without their starts
     with pytest.raises(ValueError):
         call(n_cached=torch.zeros(2, dtype=torch.int64))
@@ -89,15 +92,22 @@ def test_norm_rotary_refusals():
     call(n=0)
     assert status(lambda: call(n=-1)) == rc.RC_E_INVALID_ARG
     assert status(lambda: call(hq=3)) == rc.RC_E_INVALID_ARG
-    assert status(lambda: call(hq=8)) == rc.RC_E_INVALID_ARG                                    # rows shorter than the heads
+    assert status(lambda: call(hq=8, q=torch.zeros((3, 8, 64)))) == rc.RC_E_INVALID_ARG                                    # rows shorter than the heads
     assert status(lambda: call(eps=-1.0)) == rc.RC_E_INVALID_ARG
     assert status(lambda: call(qkv=torch.zeros((3, 8 * 64 + 6)))) == rc.RC_E_UNSUPPORTED        # stride
-    assert status(lambda: call(qkv=qkv.view(-1)[1:1 + 2 * 520].view(2, 520))) == rc.RC_E_UNSUPPORTED   # alignment
+    assert status(lambda: call(qkv=torch.zeros(3 * 520 + 1)[1:].view(3, 520))) == rc.RC_E_UNSUPPORTED   # alignment
     assert status(lambda: call(rot=rc.rc_rotary_init(rc.RC_ROTARY_HALF, 128, 1e4))) == rc.RC_E_UNSUPPORTED
     bf = rc.PagedKV.contiguous(1, 1, 16, 2, 64, rc.RC_BF16, device="cpu")
-    assert status(lambda: call(layer=bf.layer(0))) == rc.RC_E_UNSUPPORTED                       # bf16 needs heads of 128
+    assert status(lambda: call(layer=bf.layer(0), q=q.bfloat16())) == rc.RC_E_UNSUPPORTED       # bf16 needs heads of 128
     with pytest.raises(ValueError):
         call(pos=ints(0, 1))
+    with pytest.raises(ValueError):
+        call(q=q[:2])
+    with pytest.raises(ValueError):
+        call(g_q=torch.ones(64, dtype=torch.bfloat16))
+    both = torch.zeros(3 * 520 + 512)                                                           # queries over projections
+    assert status(lambda: call(qkv=both[:3 * 520].view(3, 520), q=both[3 * 520 - 256:].view(3, 4, 64)[:3])) == rc.RC_E_INVALID_ARG
+    assert status(lambda: call(k_pre=kv.k[0])) == rc.RC_E_INVALID_ARG
 
 
 def test_rotary_move_refusals():
@@ -119,11 +129,11 @@ def test_rotary_move_refusals():
 
 def test_masked_attention_refusals():
     kv = rc.PagedKV(1, 8, 4, 1, 64, rc.RC_F32, [[0, 1], [2, 3]], device="cpu")
-    q = torch.zeros((4, 2, 64))
-    out = torch.zeros_like(q)
     starts, pos = ints(0, 2, 4), ints(0, 1, 0, 1)
 
-    def call(hq=2, q=q, out=out, layer=kv.layer(0), ws=None, starts=starts, **kw):
+    def call(hq=2, q=None, out=None, layer=kv.layer(0), ws=None, starts=starts, **kw):
+        q = torch.zeros((4, max(hq, 1), 64)) if q is None else q
+        out = torch.zeros_like(q) if out is None else out
         a = dict(n_rows=4, max_rows_per_seq=2, max_len=8)
         a.update(kw)
         rc.rc_masked_attention(q, rc.MaskedAttention(starts, pos, **a), hq, layer, out, ws)
@@ -139,9 +149,16 @@ def test_masked_attention_refusals():
     assert status(lambda: call(cap=math.nan)) == rc.RC_E_INVALID_ARG
     assert status(lambda: call(scale=-1.0)) == rc.RC_E_INVALID_ARG
     assert status(lambda: call(hq=129)) == rc.RC_E_UNSUPPORTED
-    assert status(lambda: call(out=None)) == rc.RC_E_INVALID_ARG
     assert status(lambda: call(starts=ints(0, 1, 2, 4))) == rc.RC_E_CAPACITY                    # more sequences than the table has
     assert status(lambda: call(q=torch.zeros(4 * 128 + 1)[1:])) == rc.RC_E_UNSUPPORTED          # alignment
+    bf = rc.PagedKV(1, 8, 4, 1, 128, rc.RC_BF16, [[0, 1], [2, 3]], device="cpu")
+    q16 = torch.zeros((4, 2, 128), dtype=torch.bfloat16)
+    assert status(lambda: call(q=q16, layer=bf.layer(0), cap=4097.0)) == rc.RC_E_UNSUPPORTED
+    assert rc.lib.rc_masked_attention(None, None, 2, None, None, None, 0, None) == rc.RC_E_INVALID_ARG
+    with pytest.raises(ValueError):
+        call(q=torch.zeros((3, 2, 64)))
+    with pytest.raises(ValueError):
+        call(layer=bf.layer(0))
     with pytest.raises(ValueError):
         call(row_lo=ints(0))
     bad = torch.zeros(512, dtype=torch.uint8)

@@ -187,8 +187,24 @@ def test_long_ranges(dtype, hq, hkv, dh, seqs, size, split):
 @pytest.mark.parametrize("std,scale,cap", [(40.0, 0.0, 0.0), (40.0, 0.0, 50.0), (1.0, 3.0, 1e-3), (1.0, 1e-4, 1e6), (12.0, 1.0, 5.0)])
 def test_extreme_scores(dtype, hq, hkv, dh, std, scale, cap):
     """Scores of thousands, caps far below and far above the scores."""
+    if dtype == "bf16":
+        cap = min(cap, 4096.0)                                  # the largest that bf16 takes
     b = Batch(dtype, hq, hkv, dh, [(20, 70), (100, 1)], 16, seed=4, std=std)
     b.check(b.run(cap=cap, scale=scale), cap=cap, scale=scale)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 40, 1, 128), ("bf16", 2, 1, 128), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("n_seq", [64, 65, 200, 4500])
+def test_many_sequences(dtype, hq, hkv, dh, n_seq):
+    """More sequences than lanes look for a row's one at a time; some without rows."""
+    rng = np.random.default_rng(n_seq)
+    seqs = [(int(c), int(n)) for c, n in zip(rng.integers(0, 20, n_seq), rng.integers(0, 4, n_seq))]
+    b = Batch(dtype, hq, hkv, dh, seqs, 8, seed=n_seq)
+    got = b.run(cap=30.0, split=n_seq < 100)
+    some = sorted(set(rng.integers(0, n_seq, 60).tolist()) | {0, n_seq - 1})
+    every, b.seqs = b.seqs, [q if s in some else (q[0], 0) for s, q in enumerate(b.seqs)]
+    b.check(got, cap=30.0)
+    assert bool((got != 5.0).any(2).all()) and sum(n for _, n in every) == got.shape[0]
 
 
 def test_block_table_rows_and_other_streams():
