@@ -242,8 +242,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        if not torch.cuda.is_available():
-            return None          # host-side argument checks need no stream
+        if not torch.cuda.is_initialized():
+            return None          # no stream but the default one (and none is needed for host-side argument checks)
         # the current stream of the current device, without the object that torch.cuda.current_stream() makes (2.6 us a call)
         return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
     return stream.cuda_stream or None
