@@ -42,7 +42,7 @@ def check_map(out, t, want, table):
 
 
 @pytest.mark.parametrize("n_seq,size,longest", [(1, 16, 1), (1, 1, 40), (3, 16, 100), (7, 24, 300), (64, 16, 33), (256, 16, 40),
-                                                (257, 5, 17), (1000, 16, 9), (3000, 64, 3)])
+                                                (257, 5, 17), (1000, 16, 9), (3000, 64, 3), (65536, 4, 2)])
 @pytest.mark.parametrize("extras", [False, True])
 def test_batch_map(n_seq, size, longest, extras):
     rng = np.random.default_rng(n_seq * 100 + size)
@@ -140,7 +140,8 @@ def assert_close(got, want, size, out_dtype, what):
 
 
 @pytest.mark.parametrize("dtype,qkv,hq,hkv,dh", [("bf16", "f32", 32, 8, 128), ("bf16", "bf16", 40, 8, 128), ("f32", "f32", 4, 2, 64),
-                                                 ("f32", "bf16", 7, 7, 128), ("bf16", "bf16", 9, 1, 128), ("f32", "f32", 1, 1, 64)])
+                                                 ("f32", "bf16", 7, 7, 128), ("bf16", "bf16", 9, 1, 128), ("f32", "f32", 1, 1, 64),
+                                                 ("bf16", "f32", 64, 64, 128), ("f32", "f32", 32, 16, 128)])
 @pytest.mark.parametrize("n,size,layout,part,scaling", [(1, 16, "half", 1, "plain"), (5, 1, "interleaved", 2, "linear"),
                                                         (67, 24, "half", 4, "turns"), (130, 1000, "interleaved", 1, "pairs"),
                                                         (33, 16, "half", 8, "pairs")])
@@ -178,6 +179,29 @@ def test_norm_rotary_rows(dtype, qkv, hq, hkv, dh, n, size, layout, part, scalin
         mine.view(-1)[torch.from_numpy(slot[ok])] = True
         rest = ~mine.cuda()[:, None, :, None].expand_as(pool)
         assert torch.equal(pool[rest], old[rest]), what       # nothing else of the cache is written
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("dim", [8, 24, 40, 56])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotated_parts_that_are_no_multiple_of_16(dtype, dh, dim, layout):
+    code = rc.RC_BF16 if dtype == "bf16" else rc.RC_F32
+    td = rc.torch_dtype(code)
+    kv, plan, freq = pool_cache(code, 4, 2, 16, dh), *rotation(layout, dim, "plain", base=1e3)
+    n, hq = 9, 6
+    rng = np.random.default_rng(dim)
+    x = torch.from_numpy(rng.standard_normal((n, (hq + 4) * dh)).astype(np.float32)).to(td).cuda()
+    q = torch.zeros((n, hq, dh), dtype=td, device="cuda")
+    pos, slot = rng.integers(0, 5000, n), rng.permutation(64)[:n]
+    rc.rc_norm_rotary_rows(x, n, hq, plan, ints(pos), ints(slot), kv.layer(0), q)
+    h = x.double().cpu().numpy().reshape(n, -1, dh)
+    for got, part, what in ((q.double().cpu().numpy(), h[:, :hq], "q"), (rows_of(kv.k[0], slot, 16), h[:, hq:hq + 2], "k")):
+        want, room = ref.rotate(part, pos, freq, layout)
+        assert_close(got, want, room, td, what)
+    moved = pool_cache(code, 4, 2, 16, dh)
+    rc.rc_rotary_move(kv.layer(0), ints(slot), moved.layer(0), ints(slot[::-1].copy()), n, plan, ints(pos[::-1].copy()), ints(pos))
+    want, room = ref.rotate(rows_of(kv.k[0], slot, 16), pos[::-1] - pos, freq, layout)
+    assert_close(rows_of(moved.k[0], slot[::-1].copy(), 16), want, room, td, "moved")
 
 
 def test_norm_rotary_rows_behind_the_live_ones_are_left():

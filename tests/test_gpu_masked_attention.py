@@ -96,7 +96,7 @@ SEQS = {"one": [(0, 1)], "single": [(70, 1)], "tokens": [(0, 1), (62, 1), (63, 1
 
 @pytest.mark.parametrize("dtype,hq,hkv,dh", HEADS)
 @pytest.mark.parametrize("seqs", list(SEQS))
-@pytest.mark.parametrize("size,cap,bias", [(16, 0.0, False), (0, 30.0, False), (24, 0.0, True), (5, 2.0, True)])
+@pytest.mark.parametrize("size,cap,bias", [(16, 0.0, False), (0, 30.0, False), (24, 0.0, True), (5, 2.0, True), (208, 100.0, False), (24, 55.0, False)])
 def test_causal(dtype, hq, hkv, dh, seqs, size, cap, bias):
     b = Batch(dtype, hq, hkv, dh, SEQS[seqs], size, seed=hq, std=1.5)
     got = b.run(cap, bias, ranges=size != 0, slack=3)
@@ -191,6 +191,35 @@ def test_extreme_scores(dtype, hq, hkv, dh, std, scale, cap):
         cap = min(cap, 4096.0)                                  # the largest that bf16 takes
     b = Batch(dtype, hq, hkv, dh, [(20, 70), (100, 1)], 16, seed=4, std=std)
     b.check(b.run(cap=cap, scale=scale), cap=cap, scale=scale)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 8, 2, 128), ("bf16", 40, 1, 128), ("f32", 4, 2, 64)])
+def test_a_batch_without_rows(dtype, hq, hkv, dh):
+    """Bounds for rows that there are none of: nothing is written, split or not."""
+    b = Batch(dtype, hq, hkv, dh, [(300, 1), (20, 2)], 16)
+    b.run()
+    q, ws = b.keep
+    out = torch.full_like(q, 5.0)
+    for most, n in ((1, 3), (3, 3), (60, 3)):
+        plan = rc.MaskedAttention(ints([0, 0, 0]), ints([0] * 3), n, most, 301)
+        ws = rc.alloc_workspace(rc.rc_masked_attention_workspace_bytes(plan, hq, b.kv.layer(0)))
+        rc.rc_masked_attention(q, plan, hq, b.kv.layer(0), out, ws)
+        rc.rc_masked_attention(q, plan, hq, b.kv.layer(0), out)
+    assert bool((out == 5.0).all())
+
+
+def test_two_streams_at_once():
+    """Calls that overlap in time, each with a workspace of its own, give the bits of calls one after the other."""
+    many = [Batch("bf16", 8, 2, 128, [(2000 + 100 * i, 1), (500, 2)], 16, seed=i) for i in range(4)]
+    want = [b.run(cap=30.0) for b in many]
+    streams = [torch.cuda.Stream() for _ in many]
+    torch.cuda.synchronize()
+    outs = [torch.zeros_like(w) for w in want]
+    for _ in range(5):
+        for b, o, st in zip(many, outs, streams):
+            rc.rc_masked_attention(b.keep[0], b.plan, 8, b.kv.layer(0), o, b.keep[1], stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(w, o) for w, o in zip(want, outs))
 
 
 @pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 40, 1, 128), ("bf16", 2, 1, 128), ("f32", 4, 2, 64)])
