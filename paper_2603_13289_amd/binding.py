@@ -689,15 +689,16 @@ def rc_norm_rotary_rows(qkv: torch.Tensor, n: int, n_q_heads: int, rotary: rc_ro
                         g_k: Optional[torch.Tensor] = None, eps: float = 1e-5, k_pre: Optional[torch.Tensor] = None,
                         n_live: Optional[torch.Tensor] = None, stream=None) -> None:
     """qkv: [rows][width], float32 or bf16, rows any multiple of 4 elements apart."""
-    td = torch_dtype(dst.dtype)
-    if qkv.dim() != 2 or qkv.stride(1) != 1 or qkv.shape[0] < n or qkv.dtype not in (torch.float32, torch.bfloat16):
+    td, dh, qd, (stride, unit) = torch_dtype(dst.dtype), dst.head_dim, qkv.dtype, qkv.stride()
+    if unit != 1 or qkv.shape[0] < n or (qd is not torch.float32 and qd is not torch.bfloat16):
         raise ValueError(f"qkv: float32 or bf16 [{n}][width] expected")
-    if q_out.dtype is not td or q_out.numel() < n * n_q_heads * dst.head_dim:
-        raise ValueError(f"q_out: {td} [{n}][{n_q_heads}][{dst.head_dim}] expected")
-    if any(g is not None and (g.dtype is not td or g.numel() != dst.head_dim) for g in (g_q, g_k)):
-        raise ValueError(f"gains: {td} [{dst.head_dim}] expected")
-    dtype = RC_BF16 if qkv.dtype is torch.bfloat16 else RC_F32
-    _check(lib.rc_norm_rotary_rows(qkv.data_ptr(), dtype, qkv.stride(0), n, _i32(n_live, 1, "n_live"), n_q_heads, _ptr(g_q),
+    if q_out.dtype is not td or q_out.numel() < n * n_q_heads * dh:
+        raise ValueError(f"q_out: {td} [{n}][{n_q_heads}][{dh}] expected")
+    for g in (g_q, g_k):
+        if g is not None and (g.dtype is not td or g.numel() != dh):
+            raise ValueError(f"gains: {td} [{dh}] expected")
+    dtype = RC_BF16 if qd is torch.bfloat16 else RC_F32
+    _check(lib.rc_norm_rotary_rows(qkv.data_ptr(), dtype, stride, n, _i32(n_live, 1, "n_live"), n_q_heads, _ptr(g_q),
                                    _ptr(g_k), eps, C.byref(rotary), _i32(pos, n, "pos"), _i32(slot, n, "slot"), C.byref(dst),
                                    _ptr(k_pre), _ptr(q_out), _stream(stream)), "rc_norm_rotary_rows")
 

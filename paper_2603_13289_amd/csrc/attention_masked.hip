@@ -25,7 +25,7 @@ typedef __attribute__((__vector_size__(4 * sizeof(unsigned)))) unsigned u32x4;  
 
 static constexpr int DH = 128;
 static constexpr int BKV = 64;            // keys per tile of the tile kernel
-static constexpr int TILE_COLS = 128;     // columns of a tile: four wavefronts, 32 each
+static constexpr int TILE_COLS = 128, WIDE_COLS = 256;   // columns of a tile: four or eight wavefronts, 32 each
 static constexpr int ROW_COLS = 32;       // columns of the few-row kernel
 static constexpr int F32_COLS = 16;       // columns of the float kernel
 static constexpr int ROW_KEYS = 32;       // keys a wavefront of it takes at a time
@@ -201,14 +201,15 @@ __device__ inline uint2 pack4(float a, float b, float c, float d) {
 
 __device__ inline void store4(bf16* p, float a, float b, float c, float d) { *reinterpret_cast<uint2*>(p) = pack4(a, b, c, d); }
 
-// ------------------------------------------------------------------ tiles of 128 columns
+// ------------------------------------------------------------------ tiles of 128 or 256 columns
 // Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
 // over the sequences (ceil(n / R) <= floor((a + n) / R) - floor(a / R) + 1).
-template <int KIND, bool GROUPED>
-__global__ void __launch_bounds__(256, 2)
+template <int KIND, bool GROUPED, int NW>
+__global__ void __launch_bounds__(64 * NW, 8 / NW)
 masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, float* __restrict__ part_o, float2* __restrict__ part_ml) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];   // two K tiles, two V tiles
   __shared__ int bad_v;
+  constexpr int COLS = 32 * NW, STEP = 4 * NW, PER = BKV / STEP;   // columns; rows that the threads load at a time, and how often
   const int kvh = (int)blockIdx.x % a.g.n_kv_heads;
   const int item = (int)blockIdx.x / a.g.n_kv_heads;
   const int slot = n_slots - 1 - item / sp.n_chunks, chunk = item % sp.n_chunks;   // late rows see the most keys: they go first
@@ -242,11 +243,11 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   const Range mine = range_of_row(a, row);
   const unsigned seen = mine.hi < 0 ? 0u : (unsigned)(mine.hi - mine.lo) + 1u;
 
-  // Queries come in whole rows and are handed around through the memory of the first V tiles (a wavefront's own part of it): with a lane asking for pieces of
+  // Queries come in whole rows and are handed around through the memory of the tiles to come (a wavefront's own part of it): with a lane asking for pieces of
   // its own row, a load touched 64 cache lines.
   const unsigned row_head = (unsigned)row * (unsigned)a.n_q_heads + (unsigned)head;   // below 2^31 (host)
-  unsigned char* const own_rows = lds + 2 * K_TILE + wave * 32 * KROW;
-  static_assert(TILE_COLS * KROW <= 2 * V_TILE, "room for the queries");
+  unsigned char* const own_rows = lds + wave * 32 * KROW;
+  static_assert(COLS * KROW <= kTileBytes, "room for the queries");
   auto row_at = [&](int i) __attribute__((always_inline)) { return (size_t)(unsigned)__shfl((int)row_head, 4 * i + (lane >> 4), 64) * 256 + (lane & 15) * 16; };
   u32x4 q_in[8];
 #pragma unroll
@@ -271,17 +272,17 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     return {table[min(at, last_block)], key - at * block_size};
   };
   auto row_of = [&](Asked q) __attribute__((always_inline)) { return (unsigned)(min(max(q.block, 0), pool_blocks) * head_rows + kvh) * (unsigned)block_size + q.slot; };
-  u32x4 rk[4], rv[4];
-  const unsigned lane_off = (GROUPED ? (tid >> 4) * 256 : 0) + (tid & 15) * 16;
+  u32x4 rk[PER], rv[PER];
+  const unsigned lane_off = (GROUPED ? ((tid >> 4) & 15) * 256 : 0) + (tid & 15) * 16;
   auto row_bytes = [&](unsigned row, int i) __attribute__((always_inline)) -> size_t {
-    if constexpr (GROUPED) return (size_t)(unsigned)__builtin_amdgcn_readlane((int)row, 16 * i) * 256;
-    return (size_t)(unsigned)__shfl((int)row, (tid >> 4) + 16 * i, 64) * 256;
+    if constexpr (GROUPED) return (size_t)(unsigned)__builtin_amdgcn_readlane((int)row, STEP * i + 4 * (wave & ~3)) * 256;
+    return (size_t)(unsigned)__shfl((int)row, (tid >> 4) + STEP * i, 64) * 256;
   };
   auto load = [&](const char* pool, size_t at) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(pool + at + lane_off); };
   auto fetch = [&](Asked q) __attribute__((always_inline)) {
     const unsigned row = row_of(q);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < PER; ++i) {
       const size_t at = row_bytes(row, i);
       rk[i] = load(k_pool, at);
       rv[i] = load(v_pool, at);
@@ -293,16 +294,16 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   unsigned char* const v_wr = lds + 2 * K_TILE + (tid >> 4) * VROW + (tid & 15) * 16;
   auto stage_k = [&](auto buf) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<u32x4*>(k_wr + decltype(buf)::value * K_TILE + i * 16 * KROW) = rk[i];
+    for (int i = 0; i < PER; ++i) *reinterpret_cast<u32x4*>(k_wr + decltype(buf)::value * K_TILE + i * STEP * KROW) = rk[i];
   };
   auto stage_v = [&](auto buf, int i) __attribute__((always_inline)) {
-    *reinterpret_cast<u32x4*>(v_wr + decltype(buf)::value * V_TILE + i * 16 * VROW) = rv[i];
+    *reinterpret_cast<u32x4*>(v_wr + decltype(buf)::value * V_TILE + i * STEP * VROW) = rv[i];
   };
   auto clean_v = [&](int t) __attribute__((always_inline)) {
     if ((t >= t_whole && t < t_ragged) || t >= t_end) return;
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) rv[i] = only_finite(rv[i], bad);
+    for (int i = 0; i < PER; ++i) rv[i] = only_finite(rv[i], bad);
     if (bad) bad_v = 1;
   };
 
@@ -330,11 +331,11 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
     asked = ask(t_begin + 2);
     fetch(q0);
     hand_queries();
-    __syncthreads();   // the queries are in registers: V may come where they were
+    __syncthreads();   // the queries are in registers: K and V may come where they were
     clean_v(t_begin);
     stage_k(buf0);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) stage_v(buf0, i);
+    for (int i = 0; i < PER; ++i) stage_v(buf0, i);
     fetch(q1);
   }
   __syncthreads();
@@ -412,8 +413,8 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
         for (int j = 0; j < 8; ++j) weight(0, 8 * u + j);
       }
       __builtin_amdgcn_sched_barrier(0);
-      stage_v(other, 2 * u);
-      stage_v(other, 2 * u + 1);
+#pragma unroll
+      for (int i = u * PER / 2; i < (u + 1) * PER / 2; ++i) stage_v(other, i);
       __builtin_amdgcn_sched_barrier(0);
     }
     size_t at = 0;
@@ -428,11 +429,11 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
           weight(1, j);
         }
       }
-      if (i % 4 == 0) {
+      if (i % 4 == 0 && i / 4 < PER) {
         at = row_bytes(row2, i / 4);
         rk[i / 4] = load(k_pool, at);
       }
-      if (i % 4 == 2) rv[i / 4] = load(v_pool, at);
+      if (i % 4 == 2 && i / 4 < PER) rv[i / 4] = load(v_pool, at);
       __builtin_amdgcn_sched_barrier(0);
     }
     l_run += sum;
@@ -462,7 +463,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
   if (is_split) {
     if (!live) return;
-    const size_t at = ((size_t)(slot * (long)sp.n_chunks + chunk) * a.g.n_kv_heads + kvh) * TILE_COLS + col;
+    const size_t at = ((size_t)(slot * (long)sp.n_chunks + chunk) * a.g.n_kv_heads + kvh) * COLS + col;
     if (half == 0) part_ml[at] = make_float2(m_run, l_tot);
     float* const o = part_o + at * PROW + 4 * half;
 #pragma unroll
@@ -942,8 +943,12 @@ static MaskedPlan plan_masked(const MaskedAttnArgs& a, bool is_bf16) {
   MaskedPlan p;
   const int G = a.n_q_heads / a.g.n_kv_heads;
   p.rows = is_bf16 && (long)a.max_rows_per_seq * G <= ROW_COLS;
-  p.cols = !is_bf16 ? F32_COLS : p.rows ? ROW_COLS : TILE_COLS;
-  p.rows_per_tile = TILE_COLS / G;
+  // Tiles of 256 columns load and stage K and V once for eight wavefronts, and run alone on a compute unit: worth it where ranges are long and there are
+  // enough of them.  4096 rows over 8192 keys 622 -> 573 us (uncapped 533 -> 486), selected rows over 18k keys 708 -> 646; but packed documents
+  // of up to 2300 keys 143 -> 153, windows of 300 keys 183 -> 194, of 1200 417 -> 420.
+  const bool wide = (a.n_rows / (WIDE_COLS / G) + 1l) * a.g.n_kv_heads >= 256 && a.max_len >= 4096;
+  p.cols = !is_bf16 ? F32_COLS : p.rows ? ROW_COLS : wide ? WIDE_COLS : TILE_COLS;
+  p.rows_per_tile = p.cols / G;
   p.slots = !is_bf16 ? (long)a.n_rows * G / F32_COLS + a.n_seq : p.rows ? a.n_seq : a.n_rows / p.rows_per_tile + a.n_seq;
   const bool tiles = is_bf16 && !p.rows;
   const long wgs = p.slots * a.g.n_kv_heads;
@@ -962,12 +967,12 @@ size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16) {
   return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (a.g.head_dim + 4 + 2);
 }
 
-template <int KIND, bool GROUPED>
+template <int KIND, bool GROUPED, int NW>
 static hipError_t launch_tiles(const MaskedAttnArgs& a, const MaskedPlan& p, unsigned grid, float* part_o, float2* part_ml, hipStream_t st) {
   static std::atomic<unsigned long long> told{0};
-  const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<KIND, GROUPED>, kTileBytes, told);
+  const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<KIND, GROUPED, NW>, kTileBytes, told);
   if (e != hipSuccess) return e;
-  masked_attn_tile_kernel<KIND, GROUPED><<<grid, 256, kTileBytes, st>>>(a, p.split, (int)p.slots, p.rows_per_tile, part_o, part_ml);
+  masked_attn_tile_kernel<KIND, GROUPED, NW><<<grid, 64 * NW, kTileBytes, st>>>(a, p.split, (int)p.slots, p.rows_per_tile, part_o, part_ml);
   return hipGetLastError();
 }
 
@@ -982,8 +987,11 @@ static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, floa
   } else {
     // pages of 16, 32, 64, ... slots, or one block a sequence whose slots are a multiple of 16
     const bool grouped = a.g.max_blocks == 1 ? a.g.block_size % 16 == 0 : a.g.bs_shift >= 4;
-    return grouped ? launch_tiles<KIND, true>(a, p, (unsigned)grid, part_o, part_ml, st)
-                   : launch_tiles<KIND, false>(a, p, (unsigned)grid, part_o, part_ml, st);
+    if (p.cols == WIDE_COLS)
+      return grouped ? launch_tiles<KIND, true, 8>(a, p, (unsigned)grid, part_o, part_ml, st)
+                     : launch_tiles<KIND, false, 8>(a, p, (unsigned)grid, part_o, part_ml, st);
+    return grouped ? launch_tiles<KIND, true, 4>(a, p, (unsigned)grid, part_o, part_ml, st)
+                   : launch_tiles<KIND, false, 4>(a, p, (unsigned)grid, part_o, part_ml, st);
   }
   return hipGetLastError();
 }
@@ -1008,6 +1016,7 @@ hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float*
   if (e != hipSuccess || p.split.n_chunks <= 1) return e;
   const unsigned rows = (unsigned)per_row, by_seq = (unsigned)(((long)a.n_seq * a.max_rows_per_seq * a.n_q_heads + 3) / 4);
   if (p.rows) masked_attn_merge_kernel<bf16, DH, ROW_COLS, true><<<by_seq, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
+  else if (p.cols == WIDE_COLS) masked_attn_merge_kernel<bf16, DH, WIDE_COLS, false><<<rows, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
   else if (is_bf16) masked_attn_merge_kernel<bf16, DH, TILE_COLS, false><<<rows, 256, 0, st>>>(a, p.split, p.rows_per_tile, part, part_ml);
   else if (a.g.head_dim == 64) masked_attn_merge_kernel<float, 64, F32_COLS, false><<<rows, 256, 0, st>>>(a, p.split, 0, part, part_ml);
   else masked_attn_merge_kernel<float, 128, F32_COLS, false><<<rows, 256, 0, st>>>(a, p.split, 0, part, part_ml);

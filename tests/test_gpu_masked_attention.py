@@ -183,6 +183,24 @@ def test_long_ranges(dtype, hq, hkv, dh, seqs, size, split):
     b.check(b.run(cap=40.0, split=split), cap=40.0, rows=6)
 
 
+@pytest.mark.parametrize("hq,hkv,rows", [(40, 8, 2000), (32, 8, 2100), (16, 16, 4096)])
+@pytest.mark.parametrize("size,cap,bias", [(16, 50.0, False), (24, 0.0, True), (0, 100.0, False), (32, 0.0, False)])
+def test_wide_tiles(hq, hkv, rows, size, cap, bias):
+    """Enough long ranges for tiles of eight wavefronts: causal rows, windows, rows that see nothing, other documents' values that are no numbers."""
+    b = Batch("bf16", hq, hkv, 128, [(4300 - rows // 2, rows // 2), (700, 7), (0, rows - rows // 2)], size, seed=rows)
+    b.lo[1::3] = np.maximum(b.pos[1::3] - 300, 0)
+    b.lo[5::50], b.hi[5::50] = 4, 3
+    at = slice(b.starts[2], b.starts[3])
+    b.lo[at] = np.where(b.pos[at] >= 90, np.maximum(b.lo[at], 90), b.lo[at])
+    b.v[2][60:90, :, 3] = float("inf")
+    b.lo[at] = np.where((b.pos[at] >= 60) & (b.pos[at] < 90), b.hi[at] + 1, b.lo[at])
+    b.kv.write("v", 0, 2, b.v[2].cuda())
+    got = b.run(cap=cap, bias=bias, max_len=4300)
+    b.v[2][60:90, :, 3] = 0.0
+    b.check(got, cap=cap, bias=bias, rows=9)
+    assert bool((got[5::50] == 0).all())
+
+
 @pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 4, 2, 128), ("f32", 4, 2, 64)])
 @pytest.mark.parametrize("std,scale,cap", [(40.0, 0.0, 0.0), (40.0, 0.0, 50.0), (1.0, 3.0, 1e-3), (1.0, 1e-4, 1e6), (12.0, 1.0, 5.0)])
 def test_extreme_scores(dtype, hq, hkv, dh, std, scale, cap):
