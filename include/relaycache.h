@@ -496,7 +496,7 @@ RC_API rc_status rc_batch_map(const rc_batch_map_args* args, void* stream);
  * where qkv_dtype says so; rows qkv_stride elements apart, a multiple of 4) belongs to position pos[i] and slot[i].  Queries and keys
  * are RMS-normalised head by head with the gains g_q, g_k [dh] of T (NULL: left as they are), x / sqrt(mean(x^2) + eps) * g,
  * then rotated; queries go to q_out [n][Hq][dh] of T, keys and values into slot[i] of dst, keys before the rotation into slot[i] of the
- * pool k_pre (optional, dst's geometry).  Sums and rotations are of 32 bits (angles of 64), and a result is rounded once.
+ * pool k_pre (optional, dst's geometry, apart from dst's pools).  Sums and rotations are of 32 bits (angles of 64), and a result is rounded once.
  * n_live (optional, device): rows that there are, where n is only a bound (rc_batch_map: row_start + n_seq).
  * All arrays 16-byte aligned; q_out may not overlap qkv.  Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (stride, alignment, head_dim), RC_E_CAPACITY (pool of 2^31 rows). */
 RC_API rc_status rc_norm_rotary_rows(const void* qkv, int32_t qkv_dtype, int64_t qkv_stride, int32_t n, const int32_t* n_live,
@@ -517,7 +517,8 @@ RC_API rc_status rc_rotary_move(const rc_kv_layer* src, const int32_t* src_slot,
  * row_hi[i] of block-table row seq[s], and no others (one that sees none gets zeros):
  *   score = scale q.k, or cap tanh(scale q.k / cap);  score -= slopes[head] |row_pos[i] - key|;  out = softmax(score) V
  * Key ranges are cut to [0, max_len).  Causal attention is row_lo NULL (0) and row_hi NULL (row_pos); sliding windows, documents and prefixes are ranges
- * (rc_batch_map).  Keys and values outside a row's range do not touch it, whatever they hold.  q, out: [n_rows][Hq][dh] of T.
+ * (rc_batch_map).  Keys and values outside a row's range do not touch it, whatever they hold.  q, out: [n_rows][Hq][dh] of T, out
+ * may be q itself, but not overlap it otherwise.
  * workspace (optional, device, 256-byte aligned, rc_masked_attention_workspace_bytes): lets long key ranges be cut where the batch has few rows; NULL: not cut.
  * Calls that overlap in time need workspaces of their own.  A result does not depend on other sequences' rows but through how ranges are cut.
  * Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (more than 128 query heads on a key head, alignment, bf16 with a cap above 4096), RC_E_CAPACITY (max_len

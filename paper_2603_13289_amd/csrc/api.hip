@@ -1399,6 +1399,12 @@ static rc_status rotary_arg(const rc_rotary* r, int head_dim, RotaryArg* out) {
   return RC_OK;
 }
 
+static bool overlap(const void* a, long a_bytes, const void* b, long b_bytes) {
+  const char* const p = reinterpret_cast<const char*>(a);
+  const char* const q = reinterpret_cast<const char*>(b);
+  return p < q + b_bytes && q < p + a_bytes;
+}
+
 static bool aligned16(std::initializer_list<const void*> ps) {
   uintptr_t all = 0;
   for (const void* p : ps) all |= reinterpret_cast<uintptr_t>(p);
@@ -1444,11 +1450,10 @@ rc_status rc_norm_rotary_rows(const void* qkv, int32_t qkv_dtype, int64_t qkv_st
   if (qkv_dtype != RC_F32 && qkv_dtype != RC_BF16) return RC_E_INVALID_ARG;
   if (qkv_stride < (int64_t)(n_q_heads + 2 * (int64_t)dst->n_kv_heads) * dst->head_dim) return RC_E_INVALID_ARG;
   // a row's queries may not land where another row's projections wait to be read
-  const char* const in = reinterpret_cast<const char*>(qkv);
-  const char* const out = reinterpret_cast<const char*>(q_out);
-  const int64_t in_bytes = (int64_t)n * qkv_stride * (int64_t)elem_size(qkv_dtype), out_bytes = (int64_t)n * n_q_heads * dst->head_dim * (int64_t)elem_size(dst->dtype);
-  if (in < out + out_bytes && out < in + in_bytes) return RC_E_INVALID_ARG;
-  if (k_pre && (k_pre == dst->k || k_pre == dst->v)) return RC_E_INVALID_ARG;
+  if (overlap(qkv, (long)n * qkv_stride * (long)elem_size(qkv_dtype), q_out, (long)n * n_q_heads * dst->head_dim * (long)elem_size(dst->dtype)))
+    return RC_E_INVALID_ARG;
+  const long pool_bytes = (long)dst->n_blocks * dst->n_kv_heads * dst->block_size * dst->head_dim * (long)elem_size(dst->dtype);
+  if (k_pre && (overlap(k_pre, pool_bytes, dst->k, pool_bytes) || overlap(k_pre, pool_bytes, dst->v, pool_bytes))) return RC_E_INVALID_ARG;
   if (qkv_stride % 4 || !aligned16({qkv, g_q, g_k, k_pre, q_out})) return RC_E_UNSUPPORTED;
   NormRotaryArgs a = {qkv, (long)qkv_stride, n, n_q_heads, n_live, g_q, g_k, eps, pos, slot, {}, dst->k, dst->v, k_pre, q_out};
   RC_TRY(slot_geom_of(*dst, &a.g));
@@ -1516,6 +1521,8 @@ rc_status rc_masked_attention(const void* q, const rc_masked_attention_args* arg
   MaskedAttnArgs a;
   RC_TRY(masked_attention_args(args, n_q_heads, cache, &a));
   if (!q || !out) return RC_E_INVALID_ARG;
+  const long bytes = (long)a.n_rows * n_q_heads * cache->head_dim * (long)elem_size(cache->dtype);
+  if (q != out && overlap(q, bytes, out, bytes)) return RC_E_INVALID_ARG;
   if (!aligned16({q, out})) return RC_E_UNSUPPORTED;
   const bool is_bf16 = cache->dtype == RC_BF16;
   if (workspace && ((reinterpret_cast<uintptr_t>(workspace) & 255u) ||

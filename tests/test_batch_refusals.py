@@ -164,3 +164,15 @@ def test_masked_attention_refusals():
     bad = torch.zeros(512, dtype=torch.uint8)
     off = (-bad.data_ptr()) % 256 + 16
     assert status(lambda: call(ws=bad[off:off + 128])) == rc.RC_E_WORKSPACE
+
+
+def test_arrays_that_overlap_in_part():
+    rot = rc.rc_rotary_init(rc.RC_ROTARY_HALF, 64, 1e4)
+    kv = rc.PagedKV(1, 8, 4, 2, 64, rc.RC_F32, [[0, 1], [2, 3]], device="cpu")
+    pos = ints(0, 1, 0, 1)
+    for pool in (kv.k[0], kv.v[0]):
+        assert status(lambda: rc.rc_norm_rotary_rows(torch.zeros((4, 512)), 4, 4, rot, pos, pos, kv.layer(0), torch.zeros((4, 4, 64)),
+                                                     k_pre=pool.reshape(-1)[64:])) == rc.RC_E_INVALID_ARG
+    both = torch.zeros(5, 4, 64)
+    for q, out in ((both[1:], both[:4]), (both[:4], both[1:])):
+        assert status(lambda: rc.rc_masked_attention(q, rc.MaskedAttention(ints(0, 2, 4), pos, 4, 2, 8), 4, kv.layer(0), out)) == rc.RC_E_INVALID_ARG
