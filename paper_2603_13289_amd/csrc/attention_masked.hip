@@ -81,8 +81,9 @@ __device__ inline SeqRows find_seq(const MaskedAttnArgs& a, int x, F place) {
 // that the line and the reference exponent's subtraction are one operation.  The cap: cap tanh(x / cap) = cap - 2 cap / (exp(2 x / cap) + 1), whose
 // quotient is the raw score (it falls as the score rises); its error of 2^-23 changes a weight by as much times the cap (kMostCap: 2^-11), where weights
 // are rounded to 2^-9 in any case.
-// Bounded scores: a cap without a bias bounds them by itself, so that its softmax needs no running maximum: with the reference exponent fixed at half
-// the cap, weights lie between 2^-120 and 2^40 up to kMostBounded, and no score has to wait for another.
+// Bounded scores: a cap without a bias bounds them by itself, so that its softmax needs no running maximum: with the reference exponent fixed at a quarter of
+// the cap, weights lie between 2^-100 and 2^60 up to kMostBounded, and no score has to wait for another; values between 2^-26 and 2^48
+// keep their digits in the products' sums, wherever the scores lie (up to a million keys).
 enum ScoreKind : int { kPlain = 0, kBias = 1, kCap = 2, kCapBias = 3, kBounded = 4 };
 static constexpr float kMostBounded = 80.f;   // log2 units: a cap of 55
 template <int KIND>
@@ -101,7 +102,7 @@ struct Score {
   }
   static __device__ __forceinline__ float none() { return kFalls ? INFINITY : -INFINITY; }   // the raw score of a key that is not seen
   static __device__ __forceinline__ float larger(float x, float y) { return kFalls ? fminf(x, y) : fmaxf(x, y); }
-  __device__ __forceinline__ float first_reference() const { return kFixed ? 0.5f * add : -INFINITY; }
+  __device__ __forceinline__ float first_reference() const { return kFixed ? 0.25f * add : -INFINITY; }
 };
 
 // Two values: halves that are not finite become zeros (they would turn a weight of 0 into NaN); bad: there was one.
@@ -189,6 +190,9 @@ __device__ __forceinline__ bf16x8 v_fragment(const unsigned char* v, int t, int 
   };
   return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(at(16 * t), at(16 * t + 8), 0, 1, 2, 3, 4, 5, 6, 7));
 }
+
+// The reference exponent that a part of a range is merged with: NaN where its sum is, so that a part whose scores are all NaN, and which has no maximum, shows.
+__device__ inline float2 part_sum(float m, float l) { return make_float2(l != l ? l : m, l); }
 
 __device__ inline void store4(float* p, float a, float b, float c, float d) { *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d); }
 
@@ -464,7 +468,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   if (is_split) {
     if (!live) return;
     const size_t at = ((size_t)(slot * (long)sp.n_chunks + chunk) * a.g.n_kv_heads + kvh) * COLS + col;
-    if (half == 0) part_ml[at] = make_float2(m_run, l_tot);
+    if (half == 0) part_ml[at] = part_sum(m_run, l_tot);
     float* const o = part_o + at * PROW + 4 * half;
 #pragma unroll
     for (int db = 0; db < 4; ++db)
@@ -627,7 +631,7 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
 
   // the four wavefronts' sums, in their order
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-  if (half == 0) ml[wave][col] = make_float2(m_run, l_tot);
+  if (half == 0) ml[wave][col] = part_sum(m_run, l_tot);
   __syncthreads();
   float m_all = ml[0][col].x;
 #pragma unroll
@@ -658,7 +662,7 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
     }
     if (is_split) {
       const size_t at = ((size_t)item * a.g.n_kv_heads + kvh) * ROW_COLS + c;
-      if (d == 0) part_ml[at] = make_float2(m, l);
+      if (d == 0) part_ml[at] = part_sum(m, l);
       *reinterpret_cast<float4*>(part_o + at * PROW + d) = o;
     } else {
       const int r = sq.r0 + c / G, h = kvh * G + c % G;
@@ -726,6 +730,7 @@ masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, co
   float m = mine ? ml.x : -INFINITY;
 #pragma unroll
   for (int k = 32; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor(m, k, 64));
+  const unsigned long long parts = __ballot(mine);
   const float w = mine ? __builtin_amdgcn_exp2f(ml.x - m) : 0.f;
   float l = mine ? ml.y * w : 0.f;
 #pragma unroll
@@ -738,8 +743,8 @@ masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, co
     for (int i = 0; i < 4; ++i) {
       const int at = c + TURNS * i + turn;
       const float by = __shfl(w, at & 63, 64);
-      // not a factor of 0: what lies there may be no number
-      if (at <= c1 && by > 0.f) { acc.x += o[i].x * by; acc.y += o[i].y * by; acc.z += o[i].z * by; acc.w += o[i].w * by; }
+      // what other parts' places hold may be no number, whatever the factor
+      if (at < 64 && (parts >> at & 1)) { acc.x += o[i].x * by; acc.y += o[i].y * by; acc.z += o[i].z * by; acc.w += o[i].w * by; }
     }
   }
 #pragma unroll
@@ -896,7 +901,7 @@ masked_attn_f32_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, float* __r
   // the wavefronts' sums, in their order
   float l_tot = l_run + __shfl_xor(l_run, 16, 64);
   l_tot += __shfl_xor(l_tot, 32, 64);
-  if (kq == 0) lds_ml[wave][qi] = make_float2(m_run, l_tot);
+  if (kq == 0) lds_ml[wave][qi] = part_sum(m_run, l_tot);
   __syncthreads();
   float m_all = -INFINITY;
 #pragma unroll
@@ -921,7 +926,7 @@ masked_attn_f32_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, float* __r
     }
     if (is_split) {
       const size_t to = ((size_t)((long)slot * sp.n_chunks + chunk) * a.g.n_kv_heads + kvh) * F32_COLS + c;
-      if (d == 0) part_ml[to] = make_float2(m, l);
+      if (d == 0) part_ml[to] = part_sum(m, l);
       store4(part_o + to * OROW + d, o[0], o[1], o[2], o[3]);
     } else {
       const long cc = first + c;

@@ -325,3 +325,54 @@ def test_garbage_on_the_device_stays_in_bounds():
     b.seqs = [(40, 1), (70, 1), (0, 1)]
     b.run(seq=[5, -5, 1 << 30], cap=3.0, bias=True)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("seqs", [[(300, 1)], [(300, 2), (3000, 1)], [(0, 301)], [(0, 70), (2000, 60)]])
+@pytest.mark.parametrize("cap", [0.0, 20.0, 100.0])
+def test_a_key_without_a_number(dtype, hq, hkv, dh, seqs, cap):
+    """One NaN among a row's keys makes its outputs NaN, wherever ranges are cut: also where it is all that a part of the range has.
+    Rows that do not see it keep their outputs."""
+    for key in (0, 32, 63, 64, 299):
+        b = Batch(dtype, hq, hkv, dh, seqs, 16, seed=key)
+        if key == 32:
+            b.hi = np.minimum(b.hi, 32)                         # the only key of its block that rows see
+        elif key == 64:
+            b.lo[::2] = np.where(b.pos[::2] > 64, 65, b.lo[::2])
+        for s, n in enumerate(b.lens):
+            if key < n:
+                b.k[s][key] = float("nan")
+                b.kv.write("k", 0, s, b.k[s].cuda())
+        got = b.run(cap=cap).float().cpu().numpy()
+        sees = (b.lo <= key) & (key <= b.hi)
+        assert np.isnan(got[sees]).all() and np.isfinite(got[~sees]).all(), key
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 8, 2, 128), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("seqs", [[(0, 90)], [(1500, 1)]])
+@pytest.mark.parametrize("cap", [50.0, 55.0, 60.0, 0.0])
+@pytest.mark.parametrize("sign,size", [(1.0, 2.0 ** 40), (-1.0, 2.0 ** -20)])
+def test_scores_at_the_cap(dtype, hq, hkv, dh, seqs, cap, sign, size):
+    """Every score at one end of what the cap lets through, large and small values: weights far from 1 leave the quotient as it is."""
+    b = Batch(dtype, hq, hkv, dh, seqs, 16, seed=2)
+    b.q = torch.full_like(b.q, 8.0)
+    for s in range(len(seqs)):
+        b.k[s] = torch.full_like(b.k[s], 8.0 * sign)
+        b.v[s] = torch.sign(b.v[s]) * (1 + b.v[s].abs() / 8) * size
+        b.kv.write("k", 0, s, b.k[s].cuda())
+        b.kv.write("v", 0, s, b.v[s].cuda())
+    b.check(b.run(cap=cap), cap=cap)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dh", [("bf16", 8, 2, 128), ("bf16", 5, 1, 128), ("f32", 33, 1, 64)])
+@pytest.mark.parametrize("seqs", [[(300, 1)], [(3000, 1), (12, 2)], [(9, 160), (0, 0), (1200, 70)]])
+@pytest.mark.parametrize("split", [True, False])
+def test_out_in_the_place_of_q(dtype, hq, hkv, dh, seqs, split):
+    b = Batch(dtype, hq, hkv, dh, seqs, 16, seed=5)
+    b.lo[::9], b.hi[::9] = 2, 1
+    want = b.run(cap=30.0, split=split, slack=2)
+    q, ws = b.keep
+    before = q.clone()
+    rc.rc_masked_attention(q, b.plan, hq, b.kv.layer(0), q, ws)
+    assert torch.equal(q[:b.n], want[:b.n])
+    assert torch.equal(q[b.n:].view(torch.uint8), before[b.n:].view(torch.uint8))
