@@ -519,7 +519,8 @@ RC_API rc_status rc_rotary_move(const rc_kv_layer* src, const int32_t* src_slot,
  * Key ranges are cut to [0, max_len).  Causal attention is row_lo NULL (0) and row_hi NULL (row_pos); sliding windows, documents and prefixes are ranges
  * (rc_batch_map).  Keys and values outside a row's range do not touch it, whatever they hold.  q, out: [n_rows][Hq][dh] of T, out
  * may be q itself, but not overlap it otherwise.
- * workspace (optional, device, 256-byte aligned, rc_masked_attention_workspace_bytes): lets long key ranges be cut where the batch has few rows; NULL: not cut.
+ * workspace (optional, device, 256-byte aligned, rc_masked_attention_workspace_bytes): lets long key ranges be cut where the batch has few rows, and long
+ * ranges of many rows go first; NULL: neither.
  * Calls that overlap in time need workspaces of their own.  A result does not depend on other sequences' rows but through how ranges are cut.
  * Errors: RC_E_INVALID_ARG, RC_E_UNSUPPORTED (more than 128 query heads on a key head, alignment, bf16 with a cap above 4096), RC_E_CAPACITY (max_len
  * beyond the block table or 2^30, n_seq, n_rows * n_q_heads or pool rows of 2^31), RC_E_WORKSPACE. */

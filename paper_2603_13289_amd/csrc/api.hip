@@ -1513,7 +1513,7 @@ static rc_status masked_attention_args(const rc_masked_attention_args* d, int32_
 size_t rc_masked_attention_workspace_bytes(const rc_masked_attention_args* args, int32_t n_q_heads, const rc_kv_layer* cache) {
   MaskedAttnArgs a;
   if (masked_attention_args(args, n_q_heads, cache, &a) != RC_OK) return 0;
-  return align_up(sizeof(float) * masked_attention_partial_floats(a, cache->dtype == RC_BF16));
+  return align_up(masked_attention_part_bytes(a, cache->dtype == RC_BF16));
 }
 
 rc_status rc_masked_attention(const void* q, const rc_masked_attention_args* args, int32_t n_q_heads, const rc_kv_layer* cache, void* out,
@@ -1526,7 +1526,7 @@ rc_status rc_masked_attention(const void* q, const rc_masked_attention_args* arg
   if (!aligned16({q, out})) return RC_E_UNSUPPORTED;
   const bool is_bf16 = cache->dtype == RC_BF16;
   if (workspace && ((reinterpret_cast<uintptr_t>(workspace) & 255u) ||
-                    sizeof(float) * masked_attention_partial_floats(a, is_bf16) > workspace_bytes))
+                    masked_attention_part_bytes(a, is_bf16) > workspace_bytes))
     return RC_E_WORKSPACE;
   if (a.n_rows == 0) return RC_OK;
   a.q = q;

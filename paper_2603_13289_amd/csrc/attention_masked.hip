@@ -206,11 +206,74 @@ __device__ inline uint2 pack4(float a, float b, float c, float d) {
 __device__ inline void store4(bf16* p, float a, float b, float c, float d) { *reinterpret_cast<uint2*>(p) = pack4(a, b, c, d); }
 
 // ------------------------------------------------------------------ tiles of 128 or 256 columns
+// A wavefront has 32 columns (queries and outputs stay in its registers) and walks over the keys in steps of 64, which the workgroup stages through
+// LDS for all of its wavefronts, double buffered.  Bound by the power that products and exponentials draw together (the clock falls to 1.7-1.85 GHz):
+// 4096 rows over 8192 keys, 32 query and 8 key heads, on 16-slot pages, 497 us without a cap (1106 TFLOP/s), 585 with one (940), 560 with a bias; packed documents of
+// 20 to 2300 keys 147 us for 16k rows (600 TFLOP/s of what is multiplied: five steps a workgroup on average, before which its look-ups, queries
+// and first tile take as long as two).
 // Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
 // over the sequences (ceil(n / R) <= floor((a + n) / R) - floor(a / R) + 1).
+struct MaskedTile { int first, n_valid, table_row, unused; };
+
+// The tiles of all slots, those with the longest ranges first, empty ones last: workgroups start in order, and a long one that starts late runs on alone (packed
+// documents of 20 to 2300 keys 147 -> 137 us).  A tile's length is taken from its first row's first key to its last row's last, in steps of a quarter of
+// an octave, inside which neighbours stay neighbours, more or less, and share K and V in the caches; the exact order inside a step is left to chance: tiles
+// do not touch each other.  One workgroup, a counting sort, 4.8 us.
+static constexpr int kMostOrdered = 4096, kOrderThreads = 1024, kOrderBins = 128;
+__global__ void __launch_bounds__(kOrderThreads)
+masked_attn_order_kernel(MaskedAttnArgs a, int n_slots, int rows_per_tile, MaskedTile* __restrict__ order) {
+  __shared__ int starts[kMostOrdered + 1], count[kOrderBins], before[kOrderBins / 64];
+  constexpr int PER = kMostOrdered / kOrderThreads;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i <= a.n_seq; i += kOrderThreads) starts[i] = row_in_batch(a, a.row_start[i]);   // n_seq < n_slots <= kMostOrdered (host)
+  if (tid < kOrderBins) count[tid] = 0;
+  __syncthreads();
+  MaskedTile tile[PER];
+  int bin[PER], rank[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int slot = tid + k * kOrderThreads;
+    if (slot >= n_slots) continue;
+    int s = 0;
+    for (int n = a.n_seq; n - s > 1;) {
+      const int m = (s + n) >> 1;
+      if (starts[m] / rows_per_tile + m <= slot) s = m; else n = m;
+    }
+    const SeqRows sq = rows_of_seq(a, s, starts[s], starts[s + 1]);
+    const int first = sq.r0 + (slot - (sq.r0 / rows_per_tile + s)) * rows_per_tile;
+    const int n_valid = first < sq.r0 ? 0 : max(min(rows_per_tile, sq.r1 - first), 0);
+    tile[k] = {first, n_valid, sq.table_row, 0};
+    bin[k] = kOrderBins - 1;
+    if (n_valid > 0) {
+      const int keys = max(range_of_row(a, first + n_valid - 1).hi - range_of_row(a, first).lo, 0);
+      bin[k] -= 1 + (int)((__float_as_uint((float)(keys + BKV)) >> 21) - (__float_as_uint((float)BKV) >> 21));   // up to 2^30 keys: 24 octaves
+    }
+    rank[k] = atomicAdd(&count[bin[k]], 1);
+  }
+  __syncthreads();
+  int upto = tid < kOrderBins ? count[tid] : 0;   // inclusive within the wavefront
+  const int own = upto;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += x;
+  }
+  if (tid < kOrderBins && lane == 63) before[wave] = upto;
+  __syncthreads();
+  if (tid < kOrderBins) {
+    for (int w = 0; w < wave; ++w) upto += before[w];
+    count[tid] = upto - own;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+    if (tid + k * kOrderThreads < n_slots) order[count[bin[k]] + rank[k]] = tile[k];
+}
+
 template <int KIND, bool GROUPED, int NW>
 __global__ void __launch_bounds__(64 * NW, 8 / NW)
-masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, float* __restrict__ part_o, float2* __restrict__ part_ml) {
+masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_per_tile, const MaskedTile* __restrict__ order, float* __restrict__ part_o,
+                        float2* __restrict__ part_ml) {
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];   // two K tiles, two V tiles
   __shared__ int bad_v;
   constexpr int COLS = 32 * NW, STEP = 4 * NW, PER = BKV / STEP;   // columns; rows that the threads load at a time, and how often
@@ -218,10 +281,19 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   const int item = (int)blockIdx.x / a.g.n_kv_heads;
   const int slot = n_slots - 1 - item / sp.n_chunks, chunk = item % sp.n_chunks;   // late rows see the most keys: they go first
   const int G = a.n_q_heads / a.g.n_kv_heads;
-  const SeqRows sq = find_seq(a, slot, [&](int r0, int i) { return r0 / rows_per_tile + i; });
-  const int first = sq.r0 + (slot - (sq.r0 / rows_per_tile + sq.s)) * rows_per_tile;
-  const int n_valid = min(rows_per_tile, sq.r1 - first);
-  if (n_valid <= 0 || first < sq.r0) return;
+  int first, n_valid, table_row;
+  if (order) {
+    const MaskedTile tile = order[item];
+    first = tile.first;
+    n_valid = tile.n_valid;
+    table_row = tile.table_row;
+  } else {
+    const SeqRows sq = find_seq(a, slot, [&](int r0, int i) { return r0 / rows_per_tile + i; });
+    first = sq.r0 + (slot - (sq.r0 / rows_per_tile + sq.s)) * rows_per_tile;
+    n_valid = first < sq.r0 ? 0 : min(rows_per_tile, sq.r1 - first);
+    table_row = sq.table_row;
+  }
+  if (n_valid <= 0) return;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, half = lane >> 5;
   int lo_min = INT_MAX, lo_max = 0, hi_min = INT_MAX, hi_max = -1;
@@ -264,7 +336,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   // A lane looks up the block of one key of a tile, three tiles ahead; a thread loads 16 bytes of four rows.  GROUPED: the 16 keys of a group lie one
   // behind the other, so that loads go to a group's scalar address and a constant lane offset; else every key's row is handed around.  Behind
   // the last key that one is repeated (its group).
-  const int32_t* const table = a.g.block_table + (size_t)sq.table_row * a.g.max_blocks;
+  const int32_t* const table = a.g.block_table + (size_t)table_row * a.g.max_blocks;
   const int last_key = min(t_end * BKV, a.max_len) - 1, ask_key = GROUPED ? last_key & ~15 : last_key;
   const int last_block = a.g.max_blocks - 1, block_size = a.g.block_size, head_rows = a.g.n_kv_heads, pool_blocks = a.g.n_blocks - 1;
   const KvGeom geom = a.g;
@@ -461,7 +533,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
   part_tiles(t_end);
   if (bad_v) {
     // whole tiles were not looked at and have multiplied theirs: once more does no harm
-    add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, sq.table_row, kvh, t_begin * BKV, min(t_end * BKV, a.max_len), mine, acc_o);
+    add_not_finite(reinterpret_cast<const bf16*>(a.v_pool), a.g, table_row, kvh, t_begin * BKV, min(t_end * BKV, a.max_len), mine, acc_o);
   }
 
   const float l_tot = l_run + __shfl_xor(l_run, 32, 64);
@@ -496,7 +568,8 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
 
 // ------------------------------------------------------------------ few rows a sequence: at most 32 columns
 // A workgroup takes a sequence's columns and a range of keys; its wavefronts take every fourth block of 32 keys of the range with a softmax of
-// their own and share nothing before the end.
+// their own and share nothing before the end.  Bound by HBM: K and V pass once, the products are a fifth of the time.  16 sequences of 5k to 7k keys
+// (394 MB) in 68 us, 5.8 TB/s, where a large copy reaches 6.0; one of 5k keys (21 MB) in 8.1 us, most of which is the chain of look-ups and loads.
 static constexpr int kRowWaveBytes = ROW_KEYS * (KROW + VROW);   // a wavefront's K and V, at the end its sums
 static_assert(kRowWaveBytes >= ROW_COLS * PROW * 4, "room for the sums");
 template <int KIND>
@@ -676,7 +749,7 @@ masked_attn_rows_kernel(MaskedAttnArgs a, MaskedSplit sp, float* __restrict__ pa
 // ------------------------------------------------------------------ merge of the chunks
 // A wavefront per (row, head); lane c has chunk c's exponent and sum, D / 4 lanes with four elements each read the outputs of every second (fourth)
 // chunk.  A chunk left a result for a column exactly if the tile's range reaches into it, which it does where the row's own range does.
-// Bound by a chain of dependent reads.  ROWS (results of the few-row kernel): what is read does not hang on the rows' places, so
+// Bound by a chain of dependent reads (4.7 us).  ROWS (results of the few-row kernel): what is read does not hang on the rows' places, so
 // that the results of the first chunks are asked for beside the row's range.
 static constexpr int kMaxChunks = 64;   // a lane each
 template <typename T, int D, int COLS, bool ROWS>
@@ -756,7 +829,7 @@ masked_attn_merge_kernel(MaskedAttnArgs a, MaskedSplit sp, int rows_per_tile, co
 // ------------------------------------------------------------------ float
 // 16 columns a workgroup on 16x16x4 matrix instructions; its wavefronts take every eighth (heads of 128: fourth) block of 16 keys of the range with a
 // softmax of their own and are merged through LDS.  Bound by latency (float models have a few hundred keys), so K and V go from memory straight to
-// registers, the next block's keys under the softmax and its values under the scores.
+// registers, the next block's keys under the softmax and its values under the scores.  384 rows over as many keys, four query and two key heads of 64: 12 us.
 //   S^T[key][column]: lane holds column lane % 16, keys 4 (lane / 16) + 0..3; O^T[d][column] += V^T[d][key] P: P's operand is S^T's result as it stands
 // The tanh is the library's: what the quotient of the bf16 kernels loses (2^-23 of the cap) shows in a float output.
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float f32x4;
@@ -939,11 +1012,11 @@ masked_attn_f32_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, float* __r
 
 // ------------------------------------------------------------------ host
 // The few-row kernel serves sequences whose columns fit 32; the grid is then (sequence, chunk), else (tile, chunk).
-// Key ranges are cut until there are as many workgroups as compute units (tiles: as run at a time, two on each), but into chunks of 256 keys at
+// Key ranges are cut until there are as many workgroups as compute units (tiles: twice that, as many as run at a time), but into chunks of 256 keys at
 // least (tiles: 512; float: eight steps of a workgroup, which the merge's launch costs): more and shorter ones cost more in the merge and in beginnings than they spread.  A token for each of 8 sequences of 16k keys: 110 us
 // with 256 workgroups wanted, 111 with 1024, 125 with 4096; of one sequence of 40k keys 44 and 48; of one of 5k keys 16.0 in chunks of 256,
 // 18.5 in chunks of 128.
-struct MaskedPlan { bool rows; long slots; int rows_per_tile, cols; MaskedSplit split; };
+struct MaskedPlan { bool rows, ordered; long slots; int rows_per_tile, cols; MaskedSplit split; };
 static MaskedPlan plan_masked(const MaskedAttnArgs& a, bool is_bf16) {
   MaskedPlan p;
   const int G = a.n_q_heads / a.g.n_kv_heads;
@@ -962,14 +1035,20 @@ static MaskedPlan plan_masked(const MaskedAttnArgs& a, bool is_bf16) {
   const long chunk = chunks <= 1 ? 0 : ((a.max_len + chunks - 1) / chunks + unit - 1) / unit * unit;
   p.split.n_chunks = chunk ? (int)((a.max_len + chunk - 1) / chunk) : 1;
   p.split.chunk = (int)chunk;
+  // Worth its launch where not all tiles run at a time and ranges do not grow with the rows anyhow.  Many tiles end together by themselves, and apart
+  // in time those of a sequence read its K and V again: 200 sequences of 200 to 800 rows 960 -> 1025 us, 64 of them 299 -> 290; where a sequence has
+  // few tiles that does not count (1000 of 20 to 60 rows 287 -> 259).
+  p.ordered = tiles && p.split.n_chunks == 1 && wgs > (wide ? 256 : 512) && (a.n_seq > 1 || a.row_lo) &&
+              p.slots <= (a.max_rows_per_seq <= 4 * p.rows_per_tile ? kMostOrdered : 2048);
   return p;
 }
 
-size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16) {
+size_t masked_attention_part_bytes(const MaskedAttnArgs& a, bool is_bf16) {
   if (a.n_rows <= 0) return 0;
   const MaskedPlan p = plan_masked(a, is_bf16);
+  if (p.ordered) return (size_t)p.slots * sizeof(MaskedTile);
   if (p.split.n_chunks <= 1) return 0;
-  return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (a.g.head_dim + 4 + 2);
+  return (size_t)p.slots * p.split.n_chunks * a.g.n_kv_heads * p.cols * (a.g.head_dim + 4 + 2) * sizeof(float);
 }
 
 template <int KIND, bool GROUPED, int NW>
@@ -977,7 +1056,9 @@ static hipError_t launch_tiles(const MaskedAttnArgs& a, const MaskedPlan& p, uns
   static std::atomic<unsigned long long> told{0};
   const hipError_t e = allow_dynamic_lds((const void*)masked_attn_tile_kernel<KIND, GROUPED, NW>, kTileBytes, told);
   if (e != hipSuccess) return e;
-  masked_attn_tile_kernel<KIND, GROUPED, NW><<<grid, 64 * NW, kTileBytes, st>>>(a, p.split, (int)p.slots, p.rows_per_tile, part_o, part_ml);
+  MaskedTile* const order = p.ordered ? reinterpret_cast<MaskedTile*>(part_o) : nullptr;
+  if (order) masked_attn_order_kernel<<<1, kOrderThreads, 0, st>>>(a, (int)p.slots, p.rows_per_tile, order);
+  masked_attn_tile_kernel<KIND, GROUPED, NW><<<grid, 64 * NW, kTileBytes, st>>>(a, p.split, (int)p.slots, p.rows_per_tile, order, part_o, part_ml);
   return hipGetLastError();
 }
 
@@ -1003,7 +1084,7 @@ static hipError_t launch_bf16(const MaskedAttnArgs& a, const MaskedPlan& p, floa
 
 hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float* part, hipStream_t st) {
   MaskedPlan p = plan_masked(a, is_bf16);
-  if (!part) p.split = {1, 0};
+  if (!part) p.split = {1, 0}, p.ordered = false;
   const long grid = p.slots * p.split.n_chunks * a.g.n_kv_heads, per_row = ((long)a.n_rows * a.n_q_heads + 3) / 4;
   if (grid > INT_MAX || per_row > INT_MAX) return hipErrorInvalidValue;
   float2* const part_ml = reinterpret_cast<float2*>(part + (size_t)grid * p.cols * (a.g.head_dim + 4));

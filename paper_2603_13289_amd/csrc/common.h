@@ -528,7 +528,7 @@ struct MaskedAttnArgs {
   float scale, cap;
 };
 constexpr float kMostCap = 4096.f;   // of bf16: Score says why
-size_t masked_attention_partial_floats(const MaskedAttnArgs& a, bool is_bf16);
+size_t masked_attention_part_bytes(const MaskedAttnArgs& a, bool is_bf16);
 hipError_t launch_masked_attention(const MaskedAttnArgs& a, bool is_bf16, float* part, hipStream_t st);
 
 template <typename T>

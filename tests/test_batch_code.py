@@ -5,6 +5,7 @@ from tests.test_few_row_code import _kernels
 
 
 @pytest.mark.parametrize("source,name,count", [("attention_masked.hip", "masked_attn_tile_kernel", 20), ("attention_masked.hip", "masked_attn_rows_kernel", 5),
+                                               ("attention_masked.hip", "masked_attn_order_kernel", 1),
                                                ("attention_masked.hip", "masked_attn_f32_kernel", 2), ("attention_masked.hip", "masked_attn_merge_kernel", 5),
                                                ("batch_rows.hip", "norm_rotary_kernel", 6), ("batch_rows.hip", "rotary_move_kernel", 3),
                                                ("batch_rows.hip", "batch_map_kernel", 1)])

@@ -376,3 +376,28 @@ def test_out_in_the_place_of_q(dtype, hq, hkv, dh, seqs, split):
     rc.rc_masked_attention(q, b.plan, hq, b.kv.layer(0), q, ws)
     assert torch.equal(q[:b.n], want[:b.n])
     assert torch.equal(q[b.n:].view(torch.uint8), before[b.n:].view(torch.uint8))
+
+
+@pytest.mark.parametrize("hq,hkv,rows,longest", [(16, 8, 4300, 900), (40, 8, 1900, 500), (71, 1, 600, 300), (32, 8, 2400, 4200)])
+@pytest.mark.parametrize("n_seq", [1, 9, 700])
+def test_tiles_in_order_of_length(hq, hkv, rows, longest, n_seq):
+    """More tiles than run at a time: a workspace changes their order and no bit, and every row is written; empty sequences, rows that see nothing."""
+    rng = np.random.default_rng(n_seq)
+    cuts = np.sort(rng.integers(0, rows + 1, n_seq - 1))
+    new = np.diff(np.concatenate([[0], cuts, [rows]]))
+    seqs = [(int(rng.integers(0, 60)), int(n)) for n in new]
+    b = Batch("bf16", hq, hkv, 128, seqs, 16, seed=rows)
+    b.lo = np.maximum(b.pos - rng.integers(0, longest, b.n), 0)
+    b.lo[::3] = b.pos[::3] // 128 * 128
+    b.lo[4::31], b.hi[4::31] = 9, 8
+    most = max(max(b.lens), 4096 if longest > 4096 else 1)
+    b.kv.block_table = torch.cat([b.kv.block_table, b.kv.block_table[:, :1].expand(-1, 4300 // 16)], 1).contiguous()
+    b.kv.max_blocks = b.kv.block_table.shape[1]
+    plain = b.run(cap=30.0, split=False, max_len=most)
+    got = b.run(cap=30.0, max_len=most)
+    assert b.keep[1].numel() >= 16
+    assert torch.equal(plain, got)
+    assert bool((got != 5.0).any(2).all()) and bool((got[4::31] == 0).all())
+    keep, some = b.seqs, set(rng.integers(0, n_seq, 12).tolist()) | {0}
+    b.seqs = [q if s in some else (q[0], 0) for s, q in enumerate(keep)]
+    b.check(got, cap=30.0, rows=4)
