@@ -209,14 +209,14 @@ __device__ inline void store4(bf16* p, float a, float b, float c, float d) { *re
 // A wavefront has 32 columns (queries and outputs stay in its registers) and walks over the keys in steps of 64, which the workgroup stages through
 // LDS for all of its wavefronts, double buffered.  Bound by the power that products and exponentials draw together (the clock falls to 1.7-1.85 GHz):
 // 4096 rows over 8192 keys, 32 query and 8 key heads, on 16-slot pages, 497 us without a cap (1106 TFLOP/s), 585 with one (940), 560 with a bias; packed documents of
-// 20 to 2300 keys 147 us for 16k rows (600 TFLOP/s of what is multiplied: five steps a workgroup on average, before which its look-ups, queries
+// up to 2300 keys, 6702 rows of 40 heads, 137 us (640 TFLOP/s of what is multiplied: ten steps a workgroup on average, before which its look-ups, queries
 // and first tile take as long as two).
 // Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
 // over the sequences (ceil(n / R) <= floor((a + n) / R) - floor(a / R) + 1).
 struct MaskedTile { int first, n_valid, table_row, unused; };
 
 // The tiles of all slots, those with the longest ranges first, empty ones last: workgroups start in order, and a long one that starts late runs on alone (packed
-// documents of 20 to 2300 keys 147 -> 137 us).  A tile's length is taken from its first row's first key to its last row's last, in steps of a quarter of
+// documents of up to 2300 keys 147 -> 137 us).  A tile's length is taken from its first row's first key to its last row's last, in steps of a quarter of
 // an octave, inside which neighbours stay neighbours, more or less, and share K and V in the caches; the exact order inside a step is left to chance: tiles
 // do not touch each other.  One workgroup, a counting sort, 4.8 us.
 static constexpr int kMostOrdered = 4096, kOrderThreads = 1024, kOrderBins = 128;
@@ -568,7 +568,7 @@ masked_attn_tile_kernel(MaskedAttnArgs a, MaskedSplit sp, int n_slots, int rows_
 
 // ------------------------------------------------------------------ few rows a sequence: at most 32 columns
 // A workgroup takes a sequence's columns and a range of keys; its wavefronts take every fourth block of 32 keys of the range with a softmax of
-// their own and share nothing before the end.  Bound by HBM: K and V pass once, the products are a fifth of the time.  16 sequences of 5k to 7k keys
+// their own and share nothing before the end.  Bound by HBM: K and V pass once, the products are a fifth of the time.  16 sequences of 1.4k to 9.5k keys
 // (394 MB) in 68 us, 5.8 TB/s, where a large copy reaches 6.0; one of 5k keys (21 MB) in 8.1 us, most of which is the chain of look-ups and loads.
 static constexpr int kRowWaveBytes = ROW_KEYS * (KROW + VROW);   // a wavefront's K and V, at the end its sums
 static_assert(kRowWaveBytes >= ROW_COLS * PROW * 4, "room for the sums");
@@ -1023,7 +1023,7 @@ static MaskedPlan plan_masked(const MaskedAttnArgs& a, bool is_bf16) {
   p.rows = is_bf16 && (long)a.max_rows_per_seq * G <= ROW_COLS;
   // Tiles of 256 columns load and stage K and V once for eight wavefronts, and run alone on a compute unit: worth it where ranges are long and there are
   // enough of them.  4096 rows over 8192 keys 622 -> 573 us (uncapped 533 -> 486), selected rows over 18k keys 708 -> 646; but packed documents
-  // of up to 2300 keys 143 -> 153, windows of 300 keys 183 -> 194, of 1200 417 -> 420.
+  // of up to 2300 keys, in no order, 143 -> 153, windows of 300 keys 183 -> 194, of 1200 417 -> 420.
   const bool wide = (a.n_rows / (WIDE_COLS / G) + 1l) * a.g.n_kv_heads >= 256 && a.max_len >= 4096;
   p.cols = !is_bf16 ? F32_COLS : p.rows ? ROW_COLS : wide ? WIDE_COLS : TILE_COLS;
   p.rows_per_tile = p.cols / G;
