@@ -209,31 +209,31 @@ __device__ inline void store4(bf16* p, float a, float b, float c, float d) { *re
 // A wavefront has 32 columns (queries and outputs stay in its registers) and walks over the keys in steps of 64, which the workgroup stages through
 // LDS for all of its wavefronts, double buffered.  Bound by the power that products and exponentials draw together (the clock falls to 1.7-1.85 GHz):
 // 4096 rows over 8192 keys, 32 query and 8 key heads, on 16-slot pages, 497 us without a cap (1106 TFLOP/s), 585 with one (940), 560 with a bias; packed documents of
-// up to 2300 keys, 6702 rows of 40 heads, 137 us (640 TFLOP/s of what is multiplied: ten steps a workgroup on average, before which its look-ups, queries
+// up to 2300 keys, 6702 rows of 40 heads, 138 us (635 TFLOP/s of what is multiplied: ten steps a workgroup on average, before which its look-ups, queries
 // and first tile take as long as two).
 // Slots: the tiles of sequence s begin at slot row_start[s] / rows_per_tile + s, which leaves room for all of them without a sum
 // over the sequences (ceil(n / R) <= floor((a + n) / R) - floor(a / R) + 1).
 struct MaskedTile { int first, n_valid, table_row, unused; };
 
 // The tiles of all slots, those with the longest ranges first, empty ones last: workgroups start in order, and a long one that starts late runs on alone (packed
-// documents of up to 2300 keys 147 -> 137 us).  A tile's length is taken from its first row's first key to its last row's last, in steps of a quarter of
-// an octave, inside which neighbours stay neighbours, more or less, and share K and V in the caches; the exact order inside a step is left to chance: tiles
-// do not touch each other.  One workgroup, a counting sort, 4.8 us.
+// documents of up to 2300 keys 147 -> 138 us).  A tile's length is taken from its first row's first key to its last row's last, in steps of a quarter of
+// an octave, inside which the later rows go first and neighbours stay neighbours, which share K and V in the caches.  One workgroup, a counting sort, 4.9 us.
 static constexpr int kMostOrdered = 4096, kOrderThreads = 1024, kOrderBins = 128;
 __global__ void __launch_bounds__(kOrderThreads)
 masked_attn_order_kernel(MaskedAttnArgs a, int n_slots, int rows_per_tile, MaskedTile* __restrict__ order) {
   __shared__ int starts[kMostOrdered + 1], count[kOrderBins], before[kOrderBins / 64];
   constexpr int PER = kMostOrdered / kOrderThreads;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  for (int i = tid; i <= a.n_seq; i += kOrderThreads) starts[i] = row_in_batch(a, a.row_start[i]);   // n_seq < n_slots <= kMostOrdered (host)
+  for (int i = tid; i <= a.n_seq; i += kOrderThreads) starts[i] = row_in_batch(a, a.row_start[i]);   // n_seq <= n_slots <= kMostOrdered (host)
   if (tid < kOrderBins) count[tid] = 0;
   __syncthreads();
   MaskedTile tile[PER];
   int bin[PER], rank[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
-    const int slot = tid + k * kOrderThreads;
-    if (slot >= n_slots) continue;
+    const int slot = n_slots - 1 - (tid + k * kOrderThreads);
+    bin[k] = -1;
+    if (slot < 0) continue;
     int s = 0;
     for (int n = a.n_seq; n - s > 1;) {
       const int m = (s + n) >> 1;
@@ -248,9 +248,13 @@ masked_attn_order_kernel(MaskedAttnArgs a, int n_slots, int rows_per_tile, Maske
       const int keys = max(range_of_row(a, first + n_valid - 1).hi - range_of_row(a, first).lo, 0);
       bin[k] -= 1 + (int)((__float_as_uint((float)(keys + BKV)) >> 21) - (__float_as_uint((float)BKV) >> 21));   // up to 2^30 keys: 24 octaves
     }
-    rank[k] = atomicAdd(&count[bin[k]], 1);
   }
-  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+    for (int at = k * kOrderThreads; at < min(n_slots, (k + 1) * kOrderThreads); at += 64) {   // a wavefront at a time
+      if (wave == (at >> 6) % (kOrderThreads / 64) && bin[k] >= 0) rank[k] = atomicAdd(&count[bin[k]], 1);
+      __syncthreads();
+    }
   int upto = tid < kOrderBins ? count[tid] : 0;   // inclusive within the wavefront
   const int own = upto;
 #pragma unroll
@@ -267,7 +271,7 @@ masked_attn_order_kernel(MaskedAttnArgs a, int n_slots, int rows_per_tile, Maske
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < PER; ++k)
-    if (tid + k * kOrderThreads < n_slots) order[count[bin[k]] + rank[k]] = tile[k];
+    if (bin[k] >= 0) order[count[bin[k]] + rank[k]] = tile[k];
 }
 
 template <int KIND, bool GROUPED, int NW>
