@@ -401,3 +401,36 @@ def test_tiles_in_order_of_length(hq, hkv, rows, longest, n_seq):
     keep, some = b.seqs, set(rng.integers(0, n_seq, 12).tolist()) | {0}
     b.seqs = [q if s in some else (q[0], 0) for s, q in enumerate(keep)]
     b.check(got, cap=30.0, rows=4)
+
+
+def test_replays_in_order_of_length():
+    """A captured call whose tiles are put in order on the device, replayed with other starts and ranges inside the bounds, against calls without an order."""
+    b = Batch("bf16", 16, 8, 128, [(30, 1500), (0, 2000), (200, 800)], 16, seed=12)
+    out = b.run(cap=20.0, slack=9)
+    plan, (q, ws) = b.plan, b.keep
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        rc.rc_masked_attention(q, plan, 16, b.kv.layer(0), out, ws)
+    for i in range(4):
+        plan.row_start.copy_(ints([0, 1500 - 400 * i, 3000 + 100 * i, 4300 - 77 * i]))
+        plan.row_lo[:4300].copy_(ints(np.maximum(b.pos - 300 * i, 0)))
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = torch.full_like(out, 5.0)
+        rc.rc_masked_attention(q, plan, 16, b.kv.layer(0), eager)
+        assert torch.equal(eager, out), i
+
+
+def test_garbage_stays_in_bounds_where_tiles_are_ordered():
+    """Starts, ranges and table entries of any value: some numbers, no fault, and rows of the batch alone are written."""
+    b = Batch("bf16", 16, 8, 128, [(30, 1500), (0, 2000), (200, 800)], 16, seed=13)
+    b.starts = np.array([-7, 1 << 30, 900, -(1 << 31)])
+    b.lo[:], b.hi[:] = -1000, 1 << 30
+    b.kv.block_table.fill_(-(1 << 30))
+    b.run(seq=[5, -5, 1 << 30], cap=3.0, bias=True)
+    assert b.keep[1].numel() >= 16
+    b.starts = np.array([4300, 100, 100, 4299])
+    b.run(cap=3.0)
+    torch.cuda.synchronize()
